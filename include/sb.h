@@ -590,6 +590,108 @@ sb_status sb_spec_round(sb_model *target, const sb_kv_cache *t_kv, int32_t t_len
                         int32_t *h_branches, void *d_ws, size_t ws_bytes,
                         hipStream_t verify_stream, hipStream_t draft_stream);
 
+/* ---- the prefix cache in 8 bits --------------------------------------- */
+
+/* Tokens that share one scale (per layer, KV head, and K or V). */
+#define SB_KV_BLOCK 64
+/* Most slots of the 8-bit part of a cache. */
+#define SB_KV_MAX_SLOTS (1 << 20)
+
+/* What a code stands for, times its block's scale. */
+typedef enum {
+  SB_KV_INT8 = 0, /* an integer in [-127, 127] */
+  SB_KV_E4M3 = 1  /* an 8-bit float, 4 exponent and 3 mantissa bits, largest 448 */
+} sb_kv_format;
+
+/* A KV cache whose older part is held in 8 bits: whole blocks of SB_KV_BLOCK
+ * committed tokens, each quantised once from its bfloat16 values, and behind
+ * them a bfloat16 tail (an sb_kv_cache with its own slots from 0) for the
+ * committed tokens that do not fill a block yet and for the tree's rows.
+ * With n_blocks blocks and tail_len tail slots the cache holds kv_len =
+ * 64 n_blocks + tail_len tokens; tail slot s is position 64 n_blocks + s.
+ *
+ * A block of K (or V) is its 64 tokens of one layer and KV head.  With amax
+ * the largest magnitude in it and top = 127 (SB_KV_INT8) or 448 (SB_KV_E4M3):
+ * scale = fl32(amax / top), code = the value of the type nearest to x top /
+ * amax, ties to even.  amax = 0 gives scale 0; a NaN or infinity in the block
+ * makes its scale NaN, which every row that attends to it then shows.
+ *
+ * k and v hold the codes in the operand order of the matrix instruction
+ * (sb_kv_quantize writes it, sb_kv_dequantize reads it), one byte per value:
+ * [n_layers][n_kv_heads][capacity / 64][64 head_dim], 16-byte aligned; the
+ * scales are float32 [n_layers][n_kv_heads][capacity / 64].  capacity is in
+ * slots, a multiple of 64, at most SB_KV_MAX_SLOTS.  head_dim 64 or 128. */
+typedef struct {
+  void *k, *v;
+  float *k_scale, *v_scale;
+  int32_t capacity;
+  int32_t format; /* sb_kv_format */
+  sb_kv_cache tail;
+} sb_quantized_kv;
+
+/* Quantises slots src_slot .. src_slot + 64 n_blocks - 1 of the bfloat16
+ * cache src into blocks block .. block + n_blocks - 1 of dst, every layer and
+ * KV head.  src_slot is a multiple of 8.  Of cfg, n_layers, n_kv_heads and
+ * head_dim count, and dtype, which must be SB_BF16 (SB_ERR_DTYPE); here and
+ * below n_heads must be a multiple of n_kv_heads.  n_blocks = 0 does nothing.
+ * src may be dst->tail; dst->tail is not touched. */
+sb_status sb_kv_quantize(const sb_model_config *cfg, const sb_kv_cache *src, int32_t src_slot,
+                         const sb_quantized_kv *dst, int32_t block, int32_t n_blocks,
+                         hipStream_t stream);
+
+/* The other way: bfloat16(fl32(code scale)) of blocks block .. block +
+ * n_blocks - 1 into slots dst_slot .. of dst (dst_slot a multiple of 8). */
+sb_status sb_kv_dequantize(const sb_model_config *cfg, const sb_quantized_kv *src, int32_t block,
+                           int32_t n_blocks, const sb_kv_cache *dst, int32_t dst_slot,
+                           hipStream_t stream);
+
+/* After a rollback (sb_kv_rollback on kv->tail with tail_len for kv_len): the
+ * tail's full blocks, tail_len / 64 of them, become blocks n_blocks .. of the
+ * 8-bit part, and the tail_len % 64 slots behind them move to the tail's
+ * front.  *h_n_blocks and *h_tail_len receive the new lengths (their token
+ * total is unchanged).  tail_len < 64 launches nothing. */
+sb_status sb_kv_commit(const sb_model_config *cfg, const sb_quantized_kv *kv, int32_t n_blocks,
+                       int32_t tail_len, int32_t *h_n_blocks, int32_t *h_tail_len,
+                       hipStream_t stream);
+
+/* Workspace bytes of sb_attend_quantized for up to max_rows rows, max_blocks
+ * blocks and max_tail_len tail slots (0 for arguments it rejects). */
+size_t sb_attend_workspace_bytes(const sb_model_config *cfg, int32_t max_rows, int32_t max_blocks,
+                                 int32_t max_tail_len);
+
+/* The branch-masked attention of one layer over such a cache: row i attends
+ * to the first n_blocks blocks, to tail slots [0, tail_len) and to the tree
+ * rows on its path root .. i, whose K/V stand in tail slots tail_len + j.
+ *   d_q: bfloat16 [n_rows][n_heads][head_dim], after RoPE;
+ *   d_out: bfloat16 [n_rows][n_heads][head_dim];
+ *   layer: which layer of the caches.
+ * softmax(q k / sqrt(head_dim)) v with float32 sums and statistics; over the
+ * 8-bit blocks, q and the softmax weights enter the products as binary16 (q
+ * scaled per row, weights to 11 bits), over the tail the weights to 16 bits.
+ * n_blocks and tail_len may be 0.  64 n_blocks <= kv->capacity, tail_len +
+ * n_rows <= kv->tail.capacity (SB_ERR_CAPACITY), tail_len + n_rows <= 65536
+ * (SB_ERR_UNSUPPORTED).  With n_blocks = 0 the 8-bit pointers are not read. */
+sb_status sb_attend_quantized(const sb_model_config *cfg, const sb_quantized_kv *kv, int32_t layer,
+                              int32_t n_blocks, int32_t tail_len, const void *d_q,
+                              const int32_t *h_parents, int32_t n_rows, void *d_out, void *d_ws,
+                              size_t ws_bytes, hipStream_t stream);
+
+/* Workspace bytes of sb_verify_forward_quantized (0 for arguments it
+ * rejects). */
+size_t sb_quantized_workspace_bytes(const sb_model *m, int32_t max_rows, int32_t max_blocks,
+                                    int32_t max_tail_len);
+
+/* sb_verify_forward with such a cache as the prefix: row i's K/V go to tail
+ * slot tail_len + i, its position is 64 n_blocks + tail_len + depth(i).
+ * Then sb_accept_resample, sb_kv_rollback(m, &kv->tail, tail_len, ...) and
+ * sb_kv_commit.  SB_BF16 models (SB_ERR_DTYPE otherwise), as the chain of
+ * kernels (SB_ERR_UNSUPPORTED with SB_FWD_PERSISTENT set); the H-RAD tap is
+ * written as by sb_verify_forward. */
+sb_status sb_verify_forward_quantized(sb_model *m, const sb_quantized_kv *kv, int32_t n_blocks,
+                                      int32_t tail_len, const int32_t *d_tokens,
+                                      const int32_t *h_parents, int32_t n_rows, float temperature,
+                                      float *d_logits, sb_row_stats *d_stats, void *d_ws,
+                                      size_t ws_bytes, hipStream_t stream);
 
 /* ---- measurement ---------------------------------------------------- */
 

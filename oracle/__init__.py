@@ -21,6 +21,8 @@ MI355X path computes, written from the paper:
 * ``oracle.spec_round`` -- one whole round of Algorithm 2: the drafting
   phase, the target's chain test over the confident drafts, Algorithm 1 at
   the branch point when the chain is accepted, and both caches rolled back;
+* ``oracle.quantized`` -- the prefix cache in 8 bits with a scale per block of 64
+  tokens, and the branch-masked attention over it;
 * ``oracle.hrad``     -- H-RAD's length predictor (Section "H-RAD"): the
   last K layers' hidden states and the new token's embedding through a
   256/64/3 ReLU MLP, s_t = argmax.
@@ -35,4 +37,4 @@ output distribution, closed forms printed in the paper, hand-worked golden
 cases).  Nothing here is "parity unpinned".
 """
 
-from . import tree, decoder, sampling, rollback, hrad, branching, drafting, spec_round  # noqa: F401
+from . import tree, decoder, sampling, rollback, hrad, branching, drafting, spec_round, quantized  # noqa: F401

@@ -35,13 +35,17 @@ EXPORTS = ("sb_status_string", "sb_version", "sb_packed_bytes", "sb_pack_weight"
            "sb_draft_sample_workspace_bytes",
            "sb_draft_round_workspace_bytes", "sb_draft_round", "sb_verify_forward_noalloc",
            "sb_model_set_forward", "sb_draft_chain", "sb_draft_branches", "sb_round_finish",
-           "sb_spec_round_workspace_bytes", "sb_spec_round")
+           "sb_spec_round_workspace_bytes", "sb_spec_round",
+           "sb_kv_quantize", "sb_kv_dequantize", "sb_kv_commit", "sb_attend_workspace_bytes",
+           "sb_attend_quantized", "sb_quantized_workspace_bytes", "sb_verify_forward_quantized")
 SB_FWD_AUTO, SB_FWD_KERNELS, SB_FWD_PERSISTENT = 0, 1, 2
 
 SB_HRAD_H1, SB_HRAD_H2, SB_HRAD_CLASSES = 256, 64, 3
 BRANCH_MODES = {"topk": 0, "iid": 1, "wor": 2}
 SB_BRANCH_MAX_K, SB_BRANCH_MAX_VOCAB = 16, 1048576
 SB_DRAFT_MAX_ROWS = 64
+KV_FORMATS = {"int8": 0, "e4m3": 1}
+SB_KV_BLOCK, SB_KV_MAX_SLOTS = 64, 1 << 20
 
 KERNEL_CLASSES = {"qkv": 0, "o": 1, "gate_up": 2, "down": 3, "lm_head": 4, "attn": 5,
                   "attn_merge": 6, "norm": 7, "stats": 8, "persist": 9}
@@ -73,6 +77,12 @@ class ModelWeights(C.Structure):
 
 class KVCache(C.Structure):
     _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("capacity", C.c_int32)]
+
+
+class QuantizedKVStruct(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("k_scale", C.c_void_p),
+                ("v_scale", C.c_void_p), ("capacity", C.c_int32), ("format", C.c_int32),
+                ("tail", KVCache)]
 
 
 class HradWeights(C.Structure):
@@ -166,6 +176,25 @@ lib.sb_spec_round.argtypes = [_vp, C.POINTER(KVCache), _i32, _vp, C.POINTER(KVCa
                               C.POINTER(RoundParams), _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp,
                               _vp, _vp, C.POINTER(_i32), C.POINTER(_i32), C.POINTER(_i32), _vp,
                               _sz, _vp, _vp]
+lib.sb_kv_quantize.restype = _i32
+lib.sb_kv_quantize.argtypes = [C.POINTER(ModelConfig), C.POINTER(KVCache), _i32,
+                               C.POINTER(QuantizedKVStruct), _i32, _i32, _vp]
+lib.sb_kv_dequantize.restype = _i32
+lib.sb_kv_dequantize.argtypes = [C.POINTER(ModelConfig), C.POINTER(QuantizedKVStruct), _i32, _i32,
+                                 C.POINTER(KVCache), _i32, _vp]
+lib.sb_kv_commit.restype = _i32
+lib.sb_kv_commit.argtypes = [C.POINTER(ModelConfig), C.POINTER(QuantizedKVStruct), _i32, _i32,
+                             C.POINTER(_i32), C.POINTER(_i32), _vp]
+lib.sb_attend_workspace_bytes.restype = _sz
+lib.sb_attend_workspace_bytes.argtypes = [C.POINTER(ModelConfig), _i32, _i32, _i32]
+lib.sb_attend_quantized.restype = _i32
+lib.sb_attend_quantized.argtypes = [C.POINTER(ModelConfig), C.POINTER(QuantizedKVStruct), _i32,
+                                    _i32, _i32, _vp, C.POINTER(_i32), _i32, _vp, _vp, _sz, _vp]
+lib.sb_quantized_workspace_bytes.restype = _sz
+lib.sb_quantized_workspace_bytes.argtypes = [_vp, _i32, _i32, _i32]
+lib.sb_verify_forward_quantized.restype = _i32
+lib.sb_verify_forward_quantized.argtypes = [_vp, C.POINTER(QuantizedKVStruct), _i32, _i32, _vp,
+                                            C.POINTER(_i32), _i32, _f, _vp, _vp, _vp, _sz, _vp]
 lib.sb_hrad_predict.restype = _i32
 lib.sb_hrad_predict.argtypes = [_vp, _vp, _i32, _i32, _vp, C.POINTER(HradWeights), _vp, _vp,
                                 _vp, _sz, _vp]
@@ -206,6 +235,17 @@ def _host_i32(a) -> tuple:
     # byref of the first element: 0.6 us, arr.ctypes.data_as() 1.1; arr keeps
     # the memory and outlives the call
     return arr, C.byref(C.c_int32.from_address(arr.__array_interface__["data"][0]))
+
+
+def _on_stream_device(stream, *tensors) -> None:
+    """The tensors' device is the stream's and the current one: a launch goes
+    to the current device, where another's memory would fault."""
+    cur = torch.cuda.current_device()
+    if stream is not None and stream.device.index != cur:
+        raise ValueError(f"the stream is on device {stream.device.index}, the current one is {cur}")
+    for t in tensors:
+        if t is not None and t.device.index != cur:
+            raise ValueError(f"a tensor is on {t.device}, the current device is {cur}")
 
 
 def make_config(shape) -> ModelConfig:
@@ -416,6 +456,102 @@ def sb_draft_sample(logits: torch.Tensor, stats: torch.Tensor, src_rows, tempera
            "sb_draft_sample")
 
 
+def attention_config(n_layers: int, n_heads: int, n_kv_heads: int, head_dim: int) -> ModelConfig:
+    """A bf16 config for the calls that read the cache's sizes alone."""
+    return ModelConfig(n_layers, n_heads * head_dim, n_heads, n_kv_heads, head_dim, 8, 1, 10000.0,
+                       1e-5, SB_BF16)
+
+
+def _cache16(cfg: ModelConfig, k: torch.Tensor, v: torch.Tensor) -> KVCache:
+    """The struct of a bfloat16 cache [n_layers][n_kv][capacity][head_dim], V transposed."""
+    if k.dim() != 4 or k.shape[:2] != (cfg.n_layers, cfg.n_kv_heads) or k.shape[3] != cfg.head_dim:
+        raise ValueError("k cache must be [n_layers][n_kv][capacity][head_dim]")
+    if v.shape != (*k.shape[:2], cfg.head_dim, k.shape[2]):
+        raise ValueError("v cache must be [n_layers][n_kv][head_dim][capacity]")
+    _need(k, 0, "k", torch.bfloat16)
+    _need(v, 0, "v", torch.bfloat16)
+    return KVCache(k.data_ptr(), v.data_ptr(), k.shape[2])
+
+
+class QuantizedKV:
+    """The buffers of an sb_quantized_kv: 8-bit blocks of 64 tokens for
+    `capacity` slots (rounded up to whole blocks), their scales, and a zeroed
+    bfloat16 tail of `tail_capacity` slots (rounded up to a multiple of 8; the
+    tree's rows go there too, so at least 64 more than its largest tree keeps
+    every commit possible)."""
+
+    def __init__(self, cfg: ModelConfig, capacity: int, tail_capacity: int, format: str = "int8",
+                 device="cuda"):
+        L, H, d = cfg.n_layers, cfg.n_kv_heads, cfg.head_dim
+        blocks = (capacity + SB_KV_BLOCK - 1) // SB_KV_BLOCK
+        tail = max(8, (tail_capacity + 7) // 8 * 8)
+        self.cfg, self.format = cfg, format
+        self.k = torch.zeros((L, H, blocks, SB_KV_BLOCK * d), dtype=torch.uint8, device=device)
+        self.v = torch.zeros_like(self.k)
+        self.k_scale = torch.zeros((L, H, blocks), dtype=torch.float32, device=device)
+        self.v_scale = torch.zeros_like(self.k_scale)
+        self.tail_k = torch.zeros((L, H, tail, d), dtype=torch.bfloat16, device=device)
+        self.tail_v = torch.zeros((L, H, d, tail), dtype=torch.bfloat16, device=device)
+        self._struct = QuantizedKVStruct(self.k.data_ptr(), self.v.data_ptr(),
+                                         self.k_scale.data_ptr(), self.v_scale.data_ptr(),
+                                         blocks * SB_KV_BLOCK, KV_FORMATS[format],
+                                         _cache16(cfg, self.tail_k, self.tail_v))
+
+    def _of(self, cfg: ModelConfig, stream, *tensors):
+        """This cache's struct for a call with cfg, once its sizes agree."""
+        c = self.cfg
+        if (cfg.n_layers, cfg.n_kv_heads, cfg.head_dim) != (c.n_layers, c.n_kv_heads, c.head_dim):
+            raise ValueError("the cache was made for another n_layers, n_kv_heads or head_dim")
+        _on_stream_device(stream, self.k, *tensors)
+        return C.byref(self._struct)
+
+
+def sb_kv_quantize(cfg: ModelConfig, k: torch.Tensor, v: torch.Tensor, src_slot: int,
+                   cache: QuantizedKV, block: int, n_blocks: int, stream=None) -> None:
+    """Slots src_slot .. of the bfloat16 cache (k, v) to blocks block .. of cache."""
+    src = _cache16(cfg, k, v)
+    _check(lib.sb_kv_quantize(C.byref(cfg), C.byref(src), src_slot, cache._of(cfg, stream, k, v),
+                              block, n_blocks, _stream(stream)), "sb_kv_quantize")
+
+
+def sb_kv_dequantize(cfg: ModelConfig, cache: QuantizedKV, block: int, n_blocks: int,
+                     k: torch.Tensor, v: torch.Tensor, dst_slot: int, stream=None) -> None:
+    """Blocks block .. of cache to slots dst_slot .. of the bfloat16 cache (k, v)."""
+    dst = _cache16(cfg, k, v)
+    _check(lib.sb_kv_dequantize(C.byref(cfg), cache._of(cfg, stream, k, v), block, n_blocks,
+                                C.byref(dst), dst_slot, _stream(stream)), "sb_kv_dequantize")
+
+
+def sb_kv_commit(cfg: ModelConfig, cache: QuantizedKV, n_blocks: int, tail_len: int,
+                 stream=None) -> tuple[int, int]:
+    """The tail's full blocks to the 8-bit part.  Returns (n_blocks, tail_len) after it."""
+    nb, tl = C.c_int32(0), C.c_int32(0)
+    _check(lib.sb_kv_commit(C.byref(cfg), cache._of(cfg, stream), n_blocks, tail_len, C.byref(nb),
+                            C.byref(tl), _stream(stream)), "sb_kv_commit")
+    return int(nb.value), int(tl.value)
+
+
+def sb_attend_workspace_bytes(cfg: ModelConfig, max_rows: int, max_blocks: int,
+                              max_tail_len: int) -> int:
+    return int(lib.sb_attend_workspace_bytes(C.byref(cfg), max_rows, max_blocks, max_tail_len))
+
+
+def sb_attend_quantized(cfg: ModelConfig, cache: QuantizedKV, layer: int, n_blocks: int,
+                        tail_len: int, q: torch.Tensor, parents, out: torch.Tensor,
+                        ws: torch.Tensor, stream=None) -> None:
+    """q and out bfloat16 [n_rows][n_heads][head_dim]; the rows' K/V stand in
+    tail slots tail_len .. of the layer."""
+    par, pp = _host_i32(parents)
+    n = len(par) * cfg.n_heads * cfg.head_dim * 2
+    _need(q, n, "q", torch.bfloat16)
+    _need(out, n, "out", torch.bfloat16)
+    _need(ws, 0, "ws")
+    _check(lib.sb_attend_quantized(C.byref(cfg), cache._of(cfg, stream, q, out, ws), layer,
+                                   n_blocks, tail_len, q.data_ptr(), pp, len(par), out.data_ptr(),
+                                   ws.data_ptr(), ws.nbytes, _stream(stream)),
+           "sb_attend_quantized")
+
+
 def sb_sample_workspace_bytes(vocab: int) -> int:
     return int(lib.sb_sample_workspace_bytes(vocab))
 
@@ -608,6 +744,29 @@ class Model:
                                              pp, len(par), temperature, logits.data_ptr(),
                                              stats.data_ptr(), _stream(stream)),
                "sb_verify_forward_noalloc")
+
+    def quantized_workspace(self, max_rows: int, max_blocks: int, max_tail_len: int) -> torch.Tensor:
+        n = int(lib.sb_quantized_workspace_bytes(self.handle, max_rows, max_blocks, max_tail_len))
+        if n == 0:
+            raise SBError(1, "sb_quantized_workspace_bytes")
+        return torch.empty(n, dtype=torch.uint8, device=self.device)
+
+    def sb_verify_forward_quantized(self, cache: QuantizedKV, n_blocks: int, tail_len: int,
+                                    tokens: torch.Tensor, parents, temperature: float,
+                                    logits: torch.Tensor, stats: torch.Tensor, ws: torch.Tensor,
+                                    stream=None) -> None:
+        par, pp = _host_i32(parents)
+        n = len(par)
+        _need(tokens, n * 4, "tokens", torch.int32)
+        _need(logits, n * self.shape.vocab * 4, "logits", torch.float32)
+        _need(stats, n * 16, "stats")
+        _need(ws, 0, "ws")
+        kv = cache._of(self.cfg, stream, tokens, logits, stats, ws)
+        _check(lib.sb_verify_forward_quantized(self.handle, kv, n_blocks, tail_len,
+                                               tokens.data_ptr(), pp, n, temperature,
+                                               logits.data_ptr(), stats.data_ptr(), ws.data_ptr(),
+                                               ws.nbytes, _stream(stream)),
+               "sb_verify_forward_quantized")
 
     def sb_timer_start(self, kernel_class: str, capacity: int) -> None:
         _check(lib.sb_timer_start(self.handle, KERNEL_CLASSES[kernel_class], capacity),

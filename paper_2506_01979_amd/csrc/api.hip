@@ -56,6 +56,8 @@ struct Layout {
   size_t xa, act, q, part_o, part_ml, xn, ss, rs, pk_table, pk_sync;
   // f32
   size_t fq, fo, fact;
+  // attention over a quantised cache: partials of both its parts
+  size_t quant_o, quant_ml;
   size_t total;
   int np, n_chunks, pk_chunks, ks_h, ks_o, ks_f;
 };
@@ -231,9 +233,84 @@ struct TimedLaunch {
     SB_TRY(expr);                   \
   } while (0)
 
+// Partials of the attention over a quantised cache: room for every call of at
+// most n_rows rows, n_blocks blocks and tail_len tail slots (ranges x rows of a
+// KV head: quant_attn_plan's ranges are at most kQuantTargetGroups over the KV
+// heads and row blocks, or 2, and a range has four steps).
+void take_quant_partials(const sb_model_config &c, int n_rows, int n_blocks, int tail_len,
+                         Layout *L) {
+  const int64_t rows = (int64_t)n_rows * (c.n_heads / c.n_kv_heads);
+  const int64_t per_block = 16 * kQuantMaxRowTiles;
+  int64_t parts = kQuantTargetGroups * (rows < per_block ? rows : per_block);
+  if (parts < 2 * c.n_kv_heads * rows) parts = 2 * c.n_kv_heads * rows;
+  const int64_t ranges = ceil_div(n_blocks, 4) + ceil_div(ceil_div(tail_len + n_rows, 32), 4);
+  if (parts > ranges * c.n_kv_heads * rows) parts = ranges * c.n_kv_heads * rows;
+  L->quant_o = L->total;
+  L->quant_ml = align_up(L->quant_o + parts * c.head_dim * sizeof(float));
+  L->total = align_up(L->quant_ml + parts * 2 * sizeof(float));
+}
+
+// The 8-bit part of a forward's cache (its 16-bit cache is then the tail).
+struct QuantPrefix {
+  const sb_quantized_kv *kv;
+  int n_blocks;
+};
+
+// Arguments of the attention over layer l of a quantised cache.
+QuantAttnArgs quant_attn_args(const sb_model_config &c, const sb_quantized_kv &kv, int l,
+                              int n_blocks, int tail_len, int n_rows, const void *q,
+                              const Meta *meta, char *ws, const Layout &L) {
+  const size_t heads = (size_t)l * c.n_kv_heads, cap_blocks = kv.capacity / SB_KV_BLOCK;
+  const size_t codes = heads * kv.capacity * c.head_dim;
+  const size_t tail = heads * kv.tail.capacity * c.head_dim;
+  const QuantAttnPlan p =
+      quant_attn_plan(c.n_kv_heads, n_blocks, tail_len + n_rows, n_rows * (c.n_heads / c.n_kv_heads));
+  QuantAttnArgs a{};
+  a.q = q;
+  a.cap_blocks = (int)cap_blocks;
+  a.n_blocks = n_blocks;
+  a.format = kv.format;
+  if (n_blocks > 0) {
+    a.k8 = (const uint8_t *)kv.k + codes;
+    a.v8 = (const uint8_t *)kv.v + codes;
+    a.k_scale = kv.k_scale + heads * cap_blocks;
+    a.v_scale = kv.v_scale + heads * cap_blocks;
+  }
+  a.tk = (const uint16_t *)kv.tail.k + tail;
+  a.tv = (const uint16_t *)kv.tail.v + tail;
+  a.tail_cap = kv.tail.capacity;
+  a.tail_len = tail_len;
+  a.n_tok = n_rows;
+  a.n_heads = c.n_heads;
+  a.n_kv = c.n_kv_heads;
+  a.head_dim = c.head_dim;
+  a.n_chunks = p.c8 + p.ct;
+  a.meta = meta;
+  a.scale = 1.0f / sqrtf((float)c.head_dim);
+  a.part_o = (float *)(ws + L.quant_o);
+  a.part_ml = (float *)(ws + L.quant_ml);
+  return a;
+}
+
+// The merge that follows it.
+AttnArgs quant_merge_args(const QuantAttnArgs &a) {
+  AttnArgs m{};
+  m.n_tok = a.n_tok;
+  m.n_heads = a.n_heads;
+  m.n_kv = a.n_kv;
+  m.head_dim = a.head_dim;
+  m.n_chunks = a.n_chunks;
+  m.part_o = a.part_o;
+  m.part_ml = a.part_ml;
+  return m;
+}
+
+// quant (nullable): the committed prefix's 8-bit blocks; kv and kv_len are
+// then the tail and its length.
 sb_status forward_bf16(sb_model *m, const sb_kv_cache *kv, int kv_len, const int32_t *tokens,
                        const TreeArg &tree, int n, float temperature, float *logits,
-                       sb_row_stats *stats, char *ws, const Layout &L, hipStream_t s) {
+                       sb_row_stats *stats, char *ws, const Layout &L, hipStream_t s,
+                       const QuantPrefix *quant = nullptr) {
   const sb_model_config &c = m->cfg;
   const int H = c.hidden, d = c.head_dim;
   Meta *meta = (Meta *)(ws + L.meta);
@@ -247,7 +324,8 @@ sb_status forward_bf16(sb_model *m, const sb_kv_cache *kv, int kv_len, const int
   float *ss = (float *)(ws + L.ss);
   float *rs = (float *)(ws + L.rs);
 
-  EmbedArgs ea = embed_args(m, tokens, h, n, kv_len, meta, rope);
+  const int prefix = quant ? quant->n_blocks * SB_KV_BLOCK : 0;
+  EmbedArgs ea = embed_args(m, tokens, h, n, prefix + kv_len, meta, rope);
   ea.gain = m->layers[0].attn_norm;
   ea.xa = xa;
   ea.rs = rs;
@@ -317,8 +395,15 @@ sb_status forward_bf16(sb_model *m, const sb_kv_cache *kv, int kv_len, const int
     SB_TIMED(SB_KC_QKV, launch_gemm(EPI_QKV, ga, gq.tiles, nullptr, s));
     aa.kc = kc;
     aa.vc = vc;
-    SB_TIMED(SB_KC_ATTN, launch_attn_bf16(aa, s));
-    SB_TIMED(SB_KC_ATTN_MERGE, launch_attn_merge_bf16(aa, xa, L.ks_o, s));
+    if (quant) {
+      const QuantAttnArgs qa =
+          quant_attn_args(c, *quant->kv, l, quant->n_blocks, kv_len, n, q, meta, ws, L);
+      SB_TIMED(SB_KC_ATTN, launch_attn_quant(qa, s));
+      SB_TIMED(SB_KC_ATTN_MERGE, launch_attn_merge_bf16(quant_merge_args(qa), xa, L.ks_o, s));
+    } else {
+      SB_TIMED(SB_KC_ATTN, launch_attn_bf16(aa, s));
+      SB_TIMED(SB_KC_ATTN_MERGE, launch_attn_merge_bf16(aa, xa, L.ks_o, s));
+    }
     ga.W = (const uint16_t *)lw.o;
     ga.X = xa;
     ga.ks = go.ks;
@@ -1333,6 +1418,196 @@ sb_status sb_kv_rollback(const sb_model *m, const sb_kv_cache *kv, int32_t kv_le
   return hip_status(launch_rollback(c.n_layers, c.n_kv_heads, kv->capacity, c.head_dim,
                                     (int)elem_bytes(c), kv->k, kv->v, kv_len, d_result, d_new_len,
                                     stream));
+}
+
+// ---- the 8-bit cache --------------------------------------------------------
+
+static sb_status check_attention_config(const sb_model_config *c) {
+  if (!c || c->n_layers <= 0 || c->n_heads <= 0 || c->n_kv_heads <= 0 ||
+      c->n_heads % c->n_kv_heads != 0)
+    return SB_ERR_INVALID_ARG;
+  if (c->dtype != SB_BF16) return SB_ERR_DTYPE;
+  if (c->head_dim != 64 && c->head_dim != 128) return SB_ERR_UNSUPPORTED;
+  // rows of query heads, and (layer, head, block) grids, in 32 bits
+  if (c->n_heads > 4096 || (int64_t)c->n_layers * c->n_kv_heads > (1 << 16))
+    return SB_ERR_UNSUPPORTED;
+  return SB_OK;
+}
+
+// A 16-bit cache with slots [from, from + n).
+static sb_status check_cache16(const sb_kv_cache *kv, int64_t from, int64_t n) {
+  if (!kv || !kv->k || !kv->v || (((uintptr_t)kv->k | (uintptr_t)kv->v) & 15) != 0)
+    return SB_ERR_INVALID_ARG;
+  if (kv->capacity <= 0 || kv->capacity % 8 != 0 || from + n > kv->capacity) return SB_ERR_CAPACITY;
+  if (kv->capacity > SB_KV_MAX_SLOTS) return SB_ERR_UNSUPPORTED;
+  return SB_OK;
+}
+
+// The 8-bit part of a cache with blocks [from, from + n).
+static sb_status check_cache8(const sb_quantized_kv *kv, int64_t from, int64_t n) {
+  if (!kv || (kv->format != SB_KV_INT8 && kv->format != SB_KV_E4M3)) return SB_ERR_INVALID_ARG;
+  if (n == 0) return SB_OK;
+  if (!kv->k || !kv->v || !kv->k_scale || !kv->v_scale ||
+      (((uintptr_t)kv->k | (uintptr_t)kv->v) & 15) != 0)
+    return SB_ERR_INVALID_ARG;
+  if (kv->capacity <= 0 || kv->capacity % SB_KV_BLOCK != 0 ||
+      from + n > kv->capacity / SB_KV_BLOCK)
+    return SB_ERR_CAPACITY;
+  if (kv->capacity > SB_KV_MAX_SLOTS) return SB_ERR_UNSUPPORTED;
+  return SB_OK;
+}
+
+static sb_status quant_kv_args(const sb_model_config *cfg, const sb_quantized_kv *kv, int32_t block,
+                               int32_t n_blocks, const sb_kv_cache *kv16, int32_t slot,
+                               QuantKvArgs *a) {
+  sb_status st = check_attention_config(cfg);
+  if (st != SB_OK) return st;
+  if (block < 0 || n_blocks < 0 || slot < 0 || slot % 8 != 0) return SB_ERR_INVALID_ARG;
+  if ((st = check_cache8(kv, block, n_blocks)) != SB_OK) return st;
+  if ((st = check_cache16(kv16, slot, (int64_t)n_blocks * SB_KV_BLOCK)) != SB_OK) return st;
+  a->k = (uint8_t *)kv->k;
+  a->v = (uint8_t *)kv->v;
+  a->k_scale = kv->k_scale;
+  a->v_scale = kv->v_scale;
+  a->cap_blocks = kv->capacity / SB_KV_BLOCK;
+  a->block = block;
+  a->n_blocks = n_blocks;
+  a->k16 = (uint16_t *)kv16->k;
+  a->v16 = (uint16_t *)kv16->v;
+  a->cap = kv16->capacity;
+  a->slot = slot;
+  a->heads = cfg->n_layers * cfg->n_kv_heads;
+  a->head_dim = cfg->head_dim;
+  a->format = kv->format;
+  return SB_OK;
+}
+
+sb_status sb_kv_quantize(const sb_model_config *cfg, const sb_kv_cache *src, int32_t src_slot,
+                         const sb_quantized_kv *dst, int32_t block, int32_t n_blocks,
+                         hipStream_t stream) {
+  QuantKvArgs a{};
+  const sb_status st = quant_kv_args(cfg, dst, block, n_blocks, src, src_slot, &a);
+  if (st != SB_OK || n_blocks == 0) return st;
+  return hip_status(launch_kv_quantize(a, stream));
+}
+
+sb_status sb_kv_dequantize(const sb_model_config *cfg, const sb_quantized_kv *src, int32_t block,
+                           int32_t n_blocks, const sb_kv_cache *dst, int32_t dst_slot,
+                           hipStream_t stream) {
+  QuantKvArgs a{};
+  const sb_status st = quant_kv_args(cfg, src, block, n_blocks, dst, dst_slot, &a);
+  if (st != SB_OK || n_blocks == 0) return st;
+  return hip_status(launch_kv_dequantize(a, stream));
+}
+
+sb_status sb_kv_commit(const sb_model_config *cfg, const sb_quantized_kv *kv, int32_t n_blocks,
+                       int32_t tail_len, int32_t *h_n_blocks, int32_t *h_tail_len,
+                       hipStream_t stream) {
+  if (!kv || !h_n_blocks || !h_tail_len || n_blocks < 0 || tail_len < 0) return SB_ERR_INVALID_ARG;
+  const int full = tail_len / SB_KV_BLOCK, rest = tail_len % SB_KV_BLOCK;
+  QuantKvArgs a{};
+  sb_status st = check_cache16(&kv->tail, 0, tail_len);
+  if (st != SB_OK) return st;
+  if ((st = quant_kv_args(cfg, kv, n_blocks, full, &kv->tail, 0, &a)) != SB_OK) return st;
+  if (full > 0) {
+    SB_TRY(launch_kv_quantize(a, stream));
+    if (rest > 0)
+      SB_TRY(launch_kv_move(a.k16, a.v16, a.heads, a.cap, a.head_dim, full * SB_KV_BLOCK, rest,
+                            stream));
+  }
+  *h_n_blocks = n_blocks + full;
+  *h_tail_len = rest;
+  return SB_OK;
+}
+
+// Workspace of the attention by itself: the tree's masks, the partials.
+static Layout attend_layout(const sb_model_config &c, int n_rows, int n_blocks, int tail_len) {
+  Layout L{};
+  L.total = align_up(sizeof(Meta));
+  take_quant_partials(c, n_rows, n_blocks, tail_len, &L);
+  return L;
+}
+
+static bool quant_sizes_ok(int64_t rows, int64_t blocks, int64_t tail_len) {
+  return rows >= 1 && rows <= SB_MAX_ROWS && blocks >= 0 && tail_len >= 0 &&
+         blocks * SB_KV_BLOCK <= SB_KV_MAX_SLOTS && tail_len + rows <= kBf16MaxKeys;
+}
+
+size_t sb_attend_workspace_bytes(const sb_model_config *cfg, int32_t max_rows, int32_t max_blocks,
+                                 int32_t max_tail_len) {
+  if (check_attention_config(cfg) != SB_OK || !quant_sizes_ok(max_rows, max_blocks, max_tail_len))
+    return 0;
+  return attend_layout(*cfg, max_rows, max_blocks, max_tail_len).total;
+}
+
+// What both attention calls check of the cache.
+static sb_status check_quant_step(const sb_quantized_kv *kv, int32_t n_blocks, int32_t tail_len,
+                                  int32_t n_rows) {
+  if (n_blocks < 0 || tail_len < 0) return SB_ERR_INVALID_ARG;
+  sb_status st = check_cache8(kv, 0, n_blocks);
+  if (st != SB_OK) return st;
+  if ((st = check_cache16(&kv->tail, tail_len, n_rows)) != SB_OK) return st;
+  return quant_sizes_ok(n_rows, n_blocks, tail_len) ? SB_OK : SB_ERR_UNSUPPORTED;
+}
+
+sb_status sb_attend_quantized(const sb_model_config *cfg, const sb_quantized_kv *kv, int32_t layer,
+                              int32_t n_blocks, int32_t tail_len, const void *d_q,
+                              const int32_t *h_parents, int32_t n_rows, void *d_out, void *d_ws,
+                              size_t ws_bytes, hipStream_t stream) {
+  if (!kv || !d_q || !d_out || !d_ws || (((uintptr_t)d_q | (uintptr_t)d_out) & 15) != 0)
+    return SB_ERR_INVALID_ARG;
+  sb_status st = check_attention_config(cfg);
+  if (st != SB_OK) return st;
+  if (layer < 0 || layer >= cfg->n_layers) return SB_ERR_INVALID_ARG;
+  TreeArg tree;
+  if ((st = check_tree(h_parents, n_rows, &tree)) != SB_OK) return st;
+  if ((st = check_quant_step(kv, n_blocks, tail_len, n_rows)) != SB_OK) return st;
+  const Layout L = attend_layout(*cfg, n_rows, n_blocks, tail_len);
+  if (ws_bytes < L.total) return SB_ERR_CAPACITY;
+  Meta *meta = (Meta *)d_ws;
+  const QuantAttnArgs a = quant_attn_args(*cfg, *kv, layer, n_blocks, tail_len, n_rows, d_q, meta,
+                                          (char *)d_ws, L);
+  SB_TRY(launch_tree_masks(meta, tree, stream));
+  SB_TRY(launch_attn_quant(a, stream));
+  return hip_status(launch_attn_merge_bf16(quant_merge_args(a), (uint16_t *)d_out, 0, stream));
+}
+
+// Workspace of a forward over a quantised cache: the forward's over its tail,
+// and the attention's partials.
+static Layout quant_forward_layout(const sb_model_config &c, int n_rows, int n_blocks, int tail_len,
+                                   bool up_to) {
+  Layout L = make_layout(c, n_rows, tail_len, up_to);
+  take_quant_partials(c, n_rows, n_blocks, tail_len, &L);
+  return L;
+}
+
+size_t sb_quantized_workspace_bytes(const sb_model *m, int32_t max_rows, int32_t max_blocks,
+                                    int32_t max_tail_len) {
+  if (!m || check_attention_config(&m->cfg) != SB_OK ||
+      !quant_sizes_ok(max_rows, max_blocks, max_tail_len))
+    return 0;
+  return quant_forward_layout(m->cfg, max_rows, max_blocks, max_tail_len, true).total;
+}
+
+sb_status sb_verify_forward_quantized(sb_model *m, const sb_quantized_kv *kv, int32_t n_blocks,
+                                      int32_t tail_len, const int32_t *d_tokens,
+                                      const int32_t *h_parents, int32_t n_rows, float temperature,
+                                      float *d_logits, sb_row_stats *d_stats, void *d_ws,
+                                      size_t ws_bytes, hipStream_t stream) {
+  if (!m || !kv || !d_tokens || !d_logits || !d_stats || !d_ws || !temperature_ok(temperature))
+    return SB_ERR_INVALID_ARG;
+  sb_status st = check_attention_config(&m->cfg);
+  if (st != SB_OK) return st;
+  TreeArg tree;
+  if ((st = check_tree(h_parents, n_rows, &tree)) != SB_OK) return st;
+  if ((st = check_quant_step(kv, n_blocks, tail_len, n_rows)) != SB_OK) return st;
+  const Layout L = quant_forward_layout(m->cfg, n_rows, n_blocks, tail_len, false);
+  if (ws_bytes < L.total) return SB_ERR_CAPACITY;
+  if (m->tap && n_rows > m->tap_rows) return SB_ERR_CAPACITY;
+  if (m->fwd_mode == SB_FWD_PERSISTENT) return SB_ERR_UNSUPPORTED;
+  const QuantPrefix quant{kv, n_blocks};
+  return forward_bf16(m, &kv->tail, tail_len, d_tokens, tree, n_rows, temperature, d_logits,
+                      d_stats, (char *)d_ws, L, stream, &quant);
 }
 
 }  // extern "C"

@@ -52,69 +52,11 @@
 // rule.
 #include <math.h>
 
-#include "sb_device.h"
+#include "sb_attn_device.h"
 #include "sb_internal_fwd.h"
 
 namespace sb {
 namespace {
-
-// Workgroup barrier for LDS traffic only (does not wait for global loads).
-__device__ __forceinline__ void lds_barrier() {
-  asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-}
-
-// Two floats to packed bf16 (round to nearest even), one instruction.
-__device__ __forceinline__ uint32_t pack_bf16x2(float lo, float hi) {
-  typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-  typedef float f32x2 __attribute__((ext_vector_type(2)));
-  const f32x2 v = {lo, hi};
-  return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, bf16x2));
-}
-
-// Max / sum over the lane pairs (l, l ^ 16) and (l, l ^ 32) with the gfx950
-// lane-swap instructions: swapping a value with itself yields, in every lane,
-// the pair's even-row and odd-row values.
-__device__ __forceinline__ float max_x16(float v) {
-  const auto r = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(uint32_t, v),
-                                                  __builtin_bit_cast(uint32_t, v), false, false);
-  return fmaxf(__builtin_bit_cast(float, (uint32_t)r[0]), __builtin_bit_cast(float, (uint32_t)r[1]));
-}
-__device__ __forceinline__ float max_x32(float v) {
-  const auto r = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, v),
-                                                  __builtin_bit_cast(uint32_t, v), false, false);
-  return fmaxf(__builtin_bit_cast(float, (uint32_t)r[0]), __builtin_bit_cast(float, (uint32_t)r[1]));
-}
-__device__ __forceinline__ float sum_x16(float v) {
-  const auto r = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(uint32_t, v),
-                                                  __builtin_bit_cast(uint32_t, v), false, false);
-  return __builtin_bit_cast(float, (uint32_t)r[0]) + __builtin_bit_cast(float, (uint32_t)r[1]);
-}
-__device__ __forceinline__ float sum_x32(float v) {
-  const auto r = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, v),
-                                                  __builtin_bit_cast(uint32_t, v), false, false);
-  return __builtin_bit_cast(float, (uint32_t)r[0]) + __builtin_bit_cast(float, (uint32_t)r[1]);
-}
-
-// Visibility of the 8 keys k0 .. k0 + 7 (k0 a multiple of 8) for a row with
-// ancestor mask anc (LDS): prefix slots are visible, tree slot kv_len + j is
-// visible when bit j is set, slots >= nkeys are not.
-__device__ __forceinline__ uint32_t visible8(const uint32_t *anc, int k0, int kv_len, int nkeys) {
-  uint32_t vis;
-  const int jt = k0 - kv_len;
-  if (jt + 8 <= 0) {
-    vis = 0xffu;
-  } else if (jt >= 0) {
-    const int wi = jt >> 5, sh = jt & 31;  // bits jt .. jt + 7 of the 256-bit mask
-    const uint64_t win = (uint64_t)anc[wi] | ((uint64_t)(wi < 7 ? anc[wi + 1] : 0u) << 32);
-    vis = (uint32_t)(win >> sh) & 0xffu;
-  } else {
-    const int pre = -jt;  // 1..7 prefix keys, then tree bits 0 ..
-    vis = ((anc[0] << pre) | ((1u << pre) - 1u)) & 0xffu;
-  }
-  const int valid = nkeys - k0;
-  if (valid < 8) vis &= valid > 0 ? (1u << valid) - 1u : 0u;
-  return vis;
-}
 
 // D: head_dim; RT: 16-row query tiles; SW: 32-key steps per
 // wave (at most).  SW = 1 halves the keys, registers and LDS of a workgroup
@@ -546,6 +488,12 @@ __global__ __launch_bounds__(64 * kAttnMaxWaves) void k_attn_rows(AttnArgs a, in
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // loads into LDS still in flight
 }
 
+// Where a merge writes column k of row t: the packed operand layout of the O
+// projection, or with ks = 0 row-major rows of `width`.
+__device__ __forceinline__ size_t merged_index(int t, int k, int width, int ks) {
+  return ks ? packed_index(t, k, ks) : (size_t)t * width + k;
+}
+
 // Combines the key ranges of one (row t, query head) and writes the
 // attention output in the packed operand layout of the O projection.  The
 // 256 threads form 4 range groups x 64 column lanes.  The partial outputs of
@@ -632,7 +580,7 @@ __global__ __launch_bounds__(256) void k_attn_merge(AttnArgs a, uint16_t *__rest
     pk.y = b[2] | ((uint32_t)b[3] << 16);
     pk.z = b[4] | ((uint32_t)b[5] << 16);
     pk.w = b[6] | ((uint32_t)b[7] << 16);
-    *(uint4 *)(out + packed_index(t, head * D + d0, ks)) = pk;
+    *(uint4 *)(out + merged_index(t, head * D + d0, a.n_heads * D, ks)) = pk;
   }
   // the last head also clears the padding columns of the packed row (the
   // GEMM reads K in whole chunks)
@@ -727,7 +675,7 @@ __global__ __launch_bounds__(kMergeThreads) void k_attn_merge_reg(AttnArgs a,
   pk.z = f2bf(o1[0] * inv) | ((uint32_t)f2bf(o1[1] * inv) << 16);
   pk.w = f2bf(o1[2] * inv) | ((uint32_t)f2bf(o1[3] * inv) << 16);
   if (!live || c0 > 0) return;
-  *(uint4 *)(out + packed_index(t, head * D + part * 8, ks)) = pk;
+  *(uint4 *)(out + merged_index(t, head * D + part * 8, a.n_heads * D, ks)) = pk;
   // the last head's threads clear the row's padding columns (the GEMM
   // reads K in whole chunks)
   if (head == a.n_heads - 1) {
@@ -822,24 +770,23 @@ hipError_t launch_merge_reg(const AttnArgs &a, uint16_t *out, int ks, hipStream_
   return hipGetLastError();
 }
 
-hipError_t launch_attn_merge_bf16(const AttnArgs &a, uint16_t *out_packed, int out_ks,
-                                  hipStream_t s) {
+hipError_t launch_attn_merge_bf16(const AttnArgs &a, uint16_t *out, int out_ks, hipStream_t s) {
   if (a.n_chunks > 512) return hipErrorInvalidValue;
   if (a.head_dim == 128 && a.n_chunks <= 4 * kMergeRanges) {
-    if (a.n_chunks <= kMergeRanges) return launch_merge_reg<128, 1>(a, out_packed, out_ks, s);
-    if (a.n_chunks <= 2 * kMergeRanges) return launch_merge_reg<128, 2>(a, out_packed, out_ks, s);
-    return launch_merge_reg<128, 4>(a, out_packed, out_ks, s);
+    if (a.n_chunks <= kMergeRanges) return launch_merge_reg<128, 1>(a, out, out_ks, s);
+    if (a.n_chunks <= 2 * kMergeRanges) return launch_merge_reg<128, 2>(a, out, out_ks, s);
+    return launch_merge_reg<128, 4>(a, out, out_ks, s);
   }
   if (a.head_dim == 64 && a.n_chunks <= 4 * kMergeRanges) {
-    if (a.n_chunks <= kMergeRanges) return launch_merge_reg<64, 1>(a, out_packed, out_ks, s);
-    if (a.n_chunks <= 2 * kMergeRanges) return launch_merge_reg<64, 2>(a, out_packed, out_ks, s);
-    return launch_merge_reg<64, 4>(a, out_packed, out_ks, s);
+    if (a.n_chunks <= kMergeRanges) return launch_merge_reg<64, 1>(a, out, out_ks, s);
+    if (a.n_chunks <= 2 * kMergeRanges) return launch_merge_reg<64, 2>(a, out, out_ks, s);
+    return launch_merge_reg<64, 4>(a, out, out_ks, s);
   }
   dim3 grid(a.n_tok, a.n_heads);
   if (a.head_dim == 128)
-    hipLaunchKernelGGL(k_attn_merge<128>, grid, dim3(256), 0, s, a, out_packed, out_ks);
+    hipLaunchKernelGGL(k_attn_merge<128>, grid, dim3(256), 0, s, a, out, out_ks);
   else if (a.head_dim == 64)
-    hipLaunchKernelGGL(k_attn_merge<64>, grid, dim3(256), 0, s, a, out_packed, out_ks);
+    hipLaunchKernelGGL(k_attn_merge<64>, grid, dim3(256), 0, s, a, out, out_ks);
   else
     return hipErrorInvalidValue;
   return hipGetLastError();

@@ -249,8 +249,63 @@ struct AttnPlan {
 };
 AttnPlan attn_plan(int n_kv, int head_dim, int nkeys, int rows);
 hipError_t launch_attn_bf16(const AttnArgs &a, hipStream_t s);
-hipError_t launch_attn_merge_bf16(const AttnArgs &a, uint16_t *out_packed, int out_ks,
-                                  hipStream_t s);
+// out: the O projection's packed operand of out_ks k-steps, or with out_ks = 0
+// row-major [n_tok][n_heads][head_dim].
+hipError_t launch_attn_merge_bf16(const AttnArgs &a, uint16_t *out, int out_ks, hipStream_t s);
+
+// ---- the 8-bit cache (k_quant_kv.hip, k_attn_quant.hip) -------------------------
+// Order of a block's codes (64 tokens x D): the bytes a lane feeds to one or
+// two matrix instructions stand together, so that a wave's load of a fragment
+// is 1 KB in a row and goes straight to registers.  Fragment c holds 16 bytes
+// of every lane l (lr = l % 16, lg = l / 16), byte b of half s:
+//   K: c = kt (D / 64) + p: key 32 (kt / 2) + 8 (lr / 4) + 4 (kt % 2) + lr % 4
+//      (so that S^T = K Q^T leaves keys 8 lg .. 8 lg + 7 of a 32-key step in
+//      lane group lg, where O^T = V^T P^T wants them), dimension
+//      64 p + 32 s + 8 lg + b;
+//   V: c = dt: dimension 16 dt + lr, key 32 s + 8 lg + b.
+// SB_KV_INT8 codes are stored plus 128.
+struct QuantKvArgs {
+  uint8_t *k, *v;             // codes, layer 0
+  float *k_scale, *v_scale;
+  int cap_blocks;             // blocks per (layer, KV head)
+  int block, n_blocks;        // the blocks of this call
+  uint16_t *k16, *v16;        // the 16-bit cache, layer 0
+  int cap, slot;              // its capacity, and the slot of the first block
+  int heads;                  // n_layers n_kv_heads
+  int head_dim, format;
+};
+hipError_t launch_kv_quantize(const QuantKvArgs &a, hipStream_t s);
+hipError_t launch_kv_dequantize(const QuantKvArgs &a, hipStream_t s);
+// Slots from .. from + n - 1 of every (layer, head) to 0 .. n - 1 (n < 64 <= from).
+hipError_t launch_kv_move(uint16_t *k, uint16_t *v, int heads, int cap, int head_dim, int from,
+                          int n, hipStream_t s);
+
+// Attention of one layer over a quantised cache.  Workgroups planned for
+// (two per compute unit), most 16-row query tiles of one, most key ranges (the
+// merge kernels take 512).
+constexpr int kQuantTargetGroups = 512;
+constexpr int kQuantMaxRowTiles = 3;
+constexpr int kQuantMaxRanges = 256;
+struct QuantAttnPlan {
+  int rt, n_rb, c8, ct;  // row tiles and row blocks; ranges of the blocks and of the tail
+};
+QuantAttnPlan quant_attn_plan(int n_kv, int n_blocks, int tail_keys, int rows);
+struct QuantAttnArgs {
+  const void *q;            // bf16 [rows][n_heads][d]
+  const uint8_t *k8, *v8;   // this layer's codes
+  const float *k_scale, *v_scale;
+  int cap_blocks, n_blocks, format;
+  const uint16_t *tk, *tv;  // this layer's tail
+  int tail_cap, tail_len;
+  int n_tok, n_heads, n_kv, head_dim;
+  int n_chunks;             // c8 + ct of the plan
+  int c8, ct, n_rb;         // filled in by the launch
+  const Meta *meta;         // ancestor masks
+  float scale;
+  float *part_o, *part_ml;  // as AttnArgs
+};
+hipError_t launch_tree_masks(Meta *meta, const TreeArg &tree, hipStream_t s);
+hipError_t launch_attn_quant(const QuantAttnArgs &a, hipStream_t s);
 
 // ---- persistent forward (k_persist.hip) ------------------------------------
 // One cooperative launch runs every layer of a bf16 verify forward: one

@@ -1,0 +1,223 @@
+"""CPU pins of the 8-bit cache's oracle, and the host checks of its entry
+points (nothing here launches: the pointers are never dereferenced)."""
+import ctypes as C
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import quantized
+
+FORMATS = ["int8", "e4m3"]
+
+
+def bf16(x):
+    return torch.from_numpy(np.asarray(x, np.float32)).bfloat16().float().numpy().astype(np.float64)
+
+
+def test_e4m3_values_against_the_type():
+    """Every finite e4m3 value is its own nearest, and the nearest of points
+    between neighbours agrees with an independent cast."""
+    every = torch.arange(256, dtype=torch.uint8).view(torch.float8_e4m3fn).double().numpy()
+    every = np.unique(every[np.isfinite(every)])
+    assert every.max() == 448.0
+    assert np.array_equal(quantized.nearest(every, "e4m3"), every)
+    mid = (every[1:] + every[:-1]) / 2
+    pts = np.concatenate([mid, every[:-1] + 0.49 * np.diff(every), every[:-1] + 0.51 * np.diff(every)])
+    ref = torch.from_numpy(pts).float().to(torch.float8_e4m3fn).double().numpy()
+    assert np.array_equal(quantized.nearest(pts, "e4m3"), ref)
+
+
+@pytest.mark.parametrize("form", FORMATS)
+def test_codes_are_the_nearest(form):
+    """No other value of the type is nearer, and float32 arithmetic in the
+    stated order gives the same codes on bfloat16 inputs."""
+    g = np.random.default_rng(3)
+    x = bf16(g.standard_normal((3, 128, 64)) * np.exp2(g.integers(-20, 20, (3, 1, 1))))
+    codes, scales = quantized.quantize(x, form)
+    grid = np.arange(-127, 128.0) if form == "int8" else np.unique(np.nan_to_num(
+        torch.arange(256, dtype=torch.uint8).view(torch.float8_e4m3fn).double().numpy()))
+    b = x.reshape(3, 2, 64, 64)
+    amax = np.abs(b).max((-2, -1))
+    y = b * quantized.TOP[form] / amax[..., None, None]
+    at = np.clip(np.searchsorted(grid, y), 1, len(grid) - 1)
+    best = np.minimum(np.abs(grid[at] - y), np.abs(grid[at - 1] - y))
+    assert np.all(np.abs(codes - y) <= best * (1 + 1e-12))
+    y32 = (b.astype(np.float32) * np.float32(quantized.TOP[form])) / amax.astype(np.float32)[..., None, None]
+    assert y32.dtype == np.float32
+    assert np.array_equal(quantized.nearest(y32.astype(np.float64), form), codes)
+    assert np.array_equal(scales, (amax.astype(np.float32) / np.float32(quantized.TOP[form])))
+
+
+@pytest.mark.parametrize("form", FORMATS)
+def test_special_blocks(form):
+    x = np.zeros((4, 64, 64))
+    x[1, 5, 7] = np.nan
+    x[2, 0, 0] = -np.inf
+    x[3, 1, 1] = -1.0
+    codes, scales = quantized.quantize(x, form)
+    assert scales[0, 0] == 0 and np.isnan(scales[1, 0]) and np.isnan(scales[2, 0])
+    assert np.all(codes[:3] == 0)
+    assert codes[3, 0, 1, 1] == -quantized.TOP[form] and scales[3, 0] == np.float32(1 / quantized.TOP[form])
+
+
+def test_commit_keeps_the_order():
+    tail = bf16(np.random.default_rng(1).standard_normal((2, 200, 64)))
+    codes, scales = quantized.quantize(tail[:, :64], "int8")
+    c, s, t, n = quantized.commit(codes, scales, tail, 150, "int8")
+    assert n == 22 and c.shape == (2, 3, 64, 64) and s.shape == (2, 3)
+    assert np.array_equal(t[:, :22], tail[:, 128:150]) and np.array_equal(t[:, 22:], tail[:, 22:])
+
+
+def test_attend_is_a_softmax():
+    g = np.random.default_rng(2)
+    q, k, v = g.standard_normal((3, 4, 64)), g.standard_normal((2, 10, 64)), g.standard_normal((2, 10, 64))
+    paths = np.array([[1, 0, 0], [1, 1, 0], [1, 0, 1]], bool)
+    out, size = quantized.attend(q, k, v, paths)
+    mask = torch.from_numpy(np.concatenate([np.ones((3, 7), bool), paths], 1))
+    ref = torch.nn.functional.scaled_dot_product_attention(
+        torch.from_numpy(q).transpose(0, 1), torch.from_numpy(k).repeat_interleave(2, 0),
+        torch.from_numpy(v).repeat_interleave(2, 0), attn_mask=mask).transpose(0, 1).numpy()
+    assert np.allclose(out, ref, rtol=1e-12, atol=1e-12)
+    assert np.all(size >= np.abs(out) - 1e-12)
+
+
+# ---- host checks ---------------------------------------------------------------
+
+@pytest.fixture(scope="module")
+def api():
+    from paper_2506_01979_amd import api as A
+    return A
+
+
+def cache(api, **kw):
+    f = dict(k=16, v=32, k_scale=4, v_scale=8, capacity=256, format=0, tk=16, tv=32, tcap=128)
+    f.update(kw)
+    return api.QuantizedKVStruct(f["k"], f["v"], f["k_scale"], f["v_scale"], f["capacity"], f["format"],
+                                 api.KVCache(f["tk"], f["tv"], f["tcap"]))
+
+
+def config(api, **kw):
+    c = api.attention_config(2, 8, 2, 128)
+    for k, v in kw.items():
+        setattr(c, k, v)
+    return C.byref(c)
+
+
+@pytest.mark.parametrize("name", ["sb_kv_quantize", "sb_kv_dequantize"])
+def test_quantize_refusals(api, name):
+    def call(cfg=None, c=None, kv=(16, 32, 512), slot=0, block=0, n=1):
+        cfg = config(api) if cfg is None else cfg
+        qkv, kv = C.byref(cache(api) if c is None else c), C.byref(api.KVCache(*kv))
+        if name == "sb_kv_quantize":
+            return api.lib.sb_kv_quantize(cfg, kv, slot, qkv, block, n, None)
+        return api.lib.sb_kv_dequantize(cfg, qkv, block, n, kv, slot, None)
+    assert call(n=0) == 0                                    # nothing to do
+    assert call(n=0, c=cache(api, k=None)) == 0
+    assert call(cfg=config(api, dtype=api.SB_F32)) == 4
+    assert call(cfg=config(api, head_dim=96)) == 6
+    assert call(cfg=config(api, n_kv_heads=3)) == 1
+    assert call(cfg=config(api, n_layers=0)) == 1
+    assert call(n=-1) == 1 and call(block=-1) == 1 and call(slot=-8) == 1
+    assert call(slot=4) == 1                                 # not a multiple of 8
+    assert call(kv=(None, 32, 512)) == 1 and call(kv=(16, 40, 512)) == 1
+    for k in ("k", "v", "k_scale", "v_scale"):
+        assert call(c=cache(api, **{k: None})) == 1
+    assert call(c=cache(api, k=24)) == 1                     # not 16-byte aligned
+    assert call(c=cache(api, format=2)) == 1
+    assert call(block=3, n=2) == 3                           # 5 blocks of a cache of 4
+    assert call(c=cache(api, capacity=200)) == 3
+    assert call(c=cache(api, capacity=(1 << 20) + 64)) == 6
+    assert call(slot=456) == 3                               # slots 456 .. 519 of 512
+    assert call(kv=(16, 32, 500)) == 3                       # capacity not a multiple of 8
+    assert call(block=2 ** 31 - 1, n=2 ** 31 - 1) == 3
+
+
+def test_commit_refusals(api):
+    nb, tl = C.c_int32(-7), C.c_int32(-7)
+
+    def call(c=None, n=0, tail=10, cfg=None, out=True):
+        return api.lib.sb_kv_commit(config(api) if cfg is None else cfg, C.byref(cache(api) if c is None else c),
+                                    n, tail, C.byref(nb) if out else None, C.byref(tl), None)
+    assert call(tail=129) == 3 and call(tail=-1) == 1 and call(n=-1) == 1 and call(out=False) == 1
+    assert call(n=4, tail=64) == 3 and call(n=3, tail=128) == 3
+    assert call(cfg=config(api, dtype=0)) == 4
+    assert (nb.value, tl.value) == (-7, -7)                  # refused calls write nothing
+    assert call(n=4, tail=63) == 0 and (nb.value, tl.value) == (4, 63)
+
+
+def test_attend_refusals(api):
+    par = (C.c_int32 * 3)(-1, 0, 1)
+    need = api.sb_attend_workspace_bytes(api.attention_config(2, 8, 2, 128), 3, 4, 100)
+    assert need > 0
+
+    def call(cfg=None, c=None, layer=1, nb=4, tail=100, q=16, p=par, n=3, out=16, ws=16, size=need):
+        return api.lib.sb_attend_quantized(config(api) if cfg is None else cfg, C.byref(cache(api) if c is None else c),
+                                           layer, nb, tail, q, p, n, out, ws, size, None)
+    assert call(q=None) == 1 and call(out=None) == 1 and call(ws=None) == 1 and call(q=24) == 1
+    assert call(layer=2) == 1 and call(layer=-1) == 1 and call(nb=-1) == 1 and call(tail=-1) == 1
+    assert call(n=0) == 1 and call(n=257) == 1
+    assert call(p=(C.c_int32 * 3)(-1, 0, 2)) == 2
+    assert call(nb=5) == 3 and call(tail=126) == 3 and call(size=need - 1) == 3
+    assert call(c=cache(api, tk=None)) == 1 and call(c=cache(api, v_scale=None)) == 1
+    assert call(cfg=config(api, dtype=0)) == 4 and call(cfg=config(api, head_dim=32)) == 6
+    assert call(c=cache(api, tcap=65536 + 64), tail=65534, size=1 << 40) == 6
+    assert api.lib.sb_verify_forward_quantized(None, C.byref(cache(api)), 4, 100, 16, par, 3, 1.0, 16, 16, 16,
+                                               1 << 40, None) == 1
+
+
+@pytest.mark.parametrize("heads,kv,d", [(12, 12, 64), (40, 40, 128), (64, 8, 128), (8, 1, 64)])
+def test_attend_workspace_serves_smaller_calls(api, heads, kv, d):
+    cfg = api.attention_config(2, heads, kv, d)
+    size = lambda *a: api.sb_attend_workspace_bytes(cfg, *a)  # noqa: E731
+    for b, t in ((0, 0), (3, 63), (128, 10), (16384, 63)):
+        least = [size(n, b, t) for n in range(1, 257)]
+        assert least == sorted(least) and least[0] > 0
+    for n in (1, 33, 49, 256):
+        for t in (0, 63, 5000):
+            least = [size(n, b, t) for b in range(0, 1000, 3)]
+            assert least == sorted(least)
+        least = [size(n, 31, t) for t in range(0, 5000, 7)]
+        assert least == sorted(least)
+    assert size(0, 1, 1) == 0 and size(257, 1, 1) == 0 and size(1, -1, 0) == 0 and size(1, 1, -1) == 0
+    assert size(1, 16385, 0) == 0 and size(1, 1, 65536) == 0
+
+
+def test_forward_refusals(api):
+    w = api.ModelWeights(1, 1, 1, (api.LayerWeights * 2)(*[api.LayerWeights(1, 1, 1, 1, 1, 1)] * 2))
+    handles = []
+    for dtype in (api.SB_BF16, api.SB_F32):
+        h = C.c_void_p()
+        c = api.ModelConfig(2, 1024, 8, 2, 128, 1024, 1000, 10000.0, 1e-5, dtype)
+        assert api.lib.sb_model_create(C.byref(c), C.byref(w), C.byref(h)) == 0
+        handles.append(h)
+    m, f32 = handles
+    par = (C.c_int32 * 3)(-1, 0, 1)
+    need = api.lib.sb_quantized_workspace_bytes(m, 3, 4, 100)
+    assert need > 0
+    assert api.lib.sb_quantized_workspace_bytes(f32, 3, 4, 100) == 0
+    assert api.lib.sb_quantized_workspace_bytes(None, 3, 4, 100) == 0
+
+    def call(m=m, c=None, nb=4, tail=100, toks=16, p=par, n=3, T=1.0, size=need):
+        return api.lib.sb_verify_forward_quantized(m, C.byref(cache(api) if c is None else c), nb, tail, toks, p, n, T,
+                                                   16, 16, 16, size, None)
+    try:
+        assert call(m=f32) == 4 and call(toks=None) == 1 and call(T=-1.0) == 1 and call(T=float("nan")) == 1
+        assert call(p=(C.c_int32 * 3)(-1, 0, 2)) == 2 and call(nb=5) == 3 and call(tail=126) == 3
+        assert call(size=need - 1) == 3 and call(n=0) == 1
+        assert api.lib.sb_model_set_forward(m, api.SB_FWD_PERSISTENT) == 0
+        assert call() == 6
+    finally:
+        for h in handles:
+            api.lib.sb_model_destroy(h)
+
+
+def test_binding_refuses_other_shapes(api):
+    cfg = api.attention_config(2, 8, 2, 128)
+    k = torch.zeros((2, 2, 64, 128), dtype=torch.bfloat16)
+    with pytest.raises(ValueError, match="v cache"):
+        api._cache16(cfg, k, k)
+    with pytest.raises(ValueError, match="k cache"):
+        api._cache16(cfg, k[:1], k)
+    with pytest.raises(ValueError, match="device"):
+        api._cache16(cfg, k, k.transpose(2, 3).contiguous())
