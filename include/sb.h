@@ -693,6 +693,57 @@ sb_status sb_verify_forward_quantized(sb_model *m, const sb_quantized_kv *kv, in
                                       float *d_logits, sb_row_stats *d_stats, void *d_ws,
                                       size_t ws_bytes, hipStream_t stream);
 
+/* ---- logits under penalties, biases and masks ------------------------- */
+
+/* Counts of n tokens: d_counts[v] (int32 [vocab]) = how often v occurs in
+ * d_tokens, added to what is there when accumulate is not 0.  Tokens outside
+ * the vocabulary are left out.  n = 0 with accumulate = 0 clears. */
+sb_status sb_count_tokens(int32_t vocab, int32_t n, const int32_t *d_tokens, int32_t accumulate,
+                          int32_t *d_counts, hipStream_t stream);
+
+/* Adds what a walk committed: the draft tokens on d_result->path (rows after
+ * the root) and d_result->next_token.  d_tokens: int32 [n_rows], the tree's
+ * tokens that the walk scored; rows outside it and tokens outside the
+ * vocabulary are left out. */
+sb_status sb_count_step(int32_t vocab, int32_t n_rows, const int32_t *d_tokens,
+                        const sb_step_result *d_result, int32_t *d_counts, hipStream_t stream);
+
+/* Rules for the logits of a token tree.  Every row has its own history: the
+ * prompt's and the output's tokens (counts of the committed tokens, the root
+ * among them) and the draft tokens on the row's path, rows 1 .. i. */
+typedef struct {
+  const int32_t *d_prompt; /* [vocab] counts, may be NULL: none */
+  const int32_t *d_output; /* [vocab] counts, may be NULL: none */
+  float repetition;        /* > 0; 1: off */
+  float presence, frequency; /* finite; 0: off */
+  const float *d_bias;     /* [vocab] added to every row, -inf bans; may be NULL */
+  const uint32_t *d_mask;  /* bit v % 32 of word v / 32: token v is allowed; may be NULL */
+  int32_t mask_stride;     /* words from a row's mask to the next row's (at least
+                              ceil(vocab / 32)); 0: one mask for all rows */
+} sb_logit_rules;
+
+/* Workspace bytes of sb_shape_logits (0 for arguments it rejects). */
+size_t sb_shape_workspace_bytes(int32_t vocab, int32_t n_rows);
+
+/* Row i of d_out = the rules applied to row i of d_logits, and its statistics
+ * at temperature T (as sb_softmax_stats; total to about 1e-7 relative).  With
+ * c = the output's count of v plus the drafts on the path that equal v, in
+ * float32, each operation rounded:
+ *   seen (c > 0 or the prompt's count > 0): l = l > 0 ? l / repetition
+ *                                             : l * repetition;
+ *   l = l - frequency * c;  c > 0: l = l - presence;  l = l + bias[v];
+ *   a token that is not allowed: -inf, whatever l was.
+ * A row with no token above -inf has NaN total at any T (SB_FLAG_NONFINITE
+ * in the walk, whose token then means nothing).  d_out may be d_logits.
+ * Between sb_verify_forward and sb_accept_resample this is what the walk
+ * tests drafts against; the draft's own rows take it before
+ * sb_draft_sample.  d_tokens int32 [n_rows]; drafts outside the vocabulary
+ * count for nothing. */
+sb_status sb_shape_logits(int32_t vocab, int32_t n_rows, const sb_logit_rules *rules,
+                          const int32_t *d_tokens, const int32_t *h_parents, const float *d_logits,
+                          float *d_out, float temperature, sb_row_stats *d_stats, void *d_ws,
+                          size_t ws_bytes, hipStream_t stream);
+
 /* ---- measurement ---------------------------------------------------- */
 
 /* Kernel classes of the verify step, for sb_timer_start. */

@@ -23,6 +23,7 @@ MI355X path computes, written from the paper:
   the branch point when the chain is accepted, and both caches rolled back;
 * ``oracle.quantized`` -- the prefix cache in 8 bits with a scale per block of 64
   tokens, and the branch-masked attention over it;
+* ``oracle.shaping``  -- penalties, biases and masks on the logits of a tree;
 * ``oracle.hrad``     -- H-RAD's length predictor (Section "H-RAD"): the
   last K layers' hidden states and the new token's embedding through a
   256/64/3 ReLU MLP, s_t = argmax.
@@ -37,4 +38,4 @@ output distribution, closed forms printed in the paper, hand-worked golden
 cases).  Nothing here is "parity unpinned".
 """
 
-from . import tree, decoder, sampling, rollback, hrad, branching, drafting, spec_round, quantized  # noqa: F401
+from . import tree, decoder, sampling, rollback, hrad, branching, drafting, spec_round, quantized, shaping  # noqa: F401

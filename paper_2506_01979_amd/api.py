@@ -37,7 +37,8 @@ EXPORTS = ("sb_status_string", "sb_version", "sb_packed_bytes", "sb_pack_weight"
            "sb_model_set_forward", "sb_draft_chain", "sb_draft_branches", "sb_round_finish",
            "sb_spec_round_workspace_bytes", "sb_spec_round",
            "sb_kv_quantize", "sb_kv_dequantize", "sb_kv_commit", "sb_attend_workspace_bytes",
-           "sb_attend_quantized", "sb_quantized_workspace_bytes", "sb_verify_forward_quantized")
+           "sb_attend_quantized", "sb_quantized_workspace_bytes", "sb_verify_forward_quantized",
+           "sb_count_tokens", "sb_count_step", "sb_shape_workspace_bytes", "sb_shape_logits")
 SB_FWD_AUTO, SB_FWD_KERNELS, SB_FWD_PERSISTENT = 0, 1, 2
 
 SB_HRAD_H1, SB_HRAD_H2, SB_HRAD_CLASSES = 256, 64, 3
@@ -83,6 +84,12 @@ class QuantizedKVStruct(C.Structure):
     _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("k_scale", C.c_void_p),
                 ("v_scale", C.c_void_p), ("capacity", C.c_int32), ("format", C.c_int32),
                 ("tail", KVCache)]
+
+
+class LogitRulesStruct(C.Structure):
+    _fields_ = [("prompt", C.c_void_p), ("output", C.c_void_p), ("repetition", C.c_float),
+                ("presence", C.c_float), ("frequency", C.c_float), ("bias", C.c_void_p),
+                ("mask", C.c_void_p), ("mask_stride", C.c_int32)]
 
 
 class HradWeights(C.Structure):
@@ -195,6 +202,15 @@ lib.sb_quantized_workspace_bytes.argtypes = [_vp, _i32, _i32, _i32]
 lib.sb_verify_forward_quantized.restype = _i32
 lib.sb_verify_forward_quantized.argtypes = [_vp, C.POINTER(QuantizedKVStruct), _i32, _i32, _vp,
                                             C.POINTER(_i32), _i32, _f, _vp, _vp, _vp, _sz, _vp]
+lib.sb_count_tokens.restype = _i32
+lib.sb_count_tokens.argtypes = [_i32, _i32, _vp, _i32, _vp, _vp]
+lib.sb_count_step.restype = _i32
+lib.sb_count_step.argtypes = [_i32, _i32, _vp, _vp, _vp, _vp]
+lib.sb_shape_workspace_bytes.restype = _sz
+lib.sb_shape_workspace_bytes.argtypes = [_i32, _i32]
+lib.sb_shape_logits.restype = _i32
+lib.sb_shape_logits.argtypes = [_i32, _i32, C.POINTER(LogitRulesStruct), _vp, C.POINTER(_i32), _vp,
+                                _vp, _f, _vp, _vp, _sz, _vp]
 lib.sb_hrad_predict.restype = _i32
 lib.sb_hrad_predict.argtypes = [_vp, _vp, _i32, _i32, _vp, C.POINTER(HradWeights), _vp, _vp,
                                 _vp, _sz, _vp]
@@ -550,6 +566,85 @@ def sb_attend_quantized(cfg: ModelConfig, cache: QuantizedKV, layer: int, n_bloc
                                    n_blocks, tail_len, q.data_ptr(), pp, len(par), out.data_ptr(),
                                    ws.data_ptr(), ws.nbytes, _stream(stream)),
            "sb_attend_quantized")
+
+
+def sb_count_tokens(tokens: torch.Tensor, counts: torch.Tensor, accumulate: bool = True,
+                    stream=None) -> None:
+    """tokens int32 [n]; counts int32 [vocab]."""
+    _need(tokens, 0, "tokens", torch.int32)
+    _need(counts, 0, "counts", torch.int32)
+    _on_stream_device(stream, tokens, counts)
+    _check(lib.sb_count_tokens(counts.numel(), tokens.numel(), tokens.data_ptr(), int(accumulate),
+                               counts.data_ptr(), _stream(stream)), "sb_count_tokens")
+
+
+def sb_count_step(tokens: torch.Tensor, result: torch.Tensor, counts: torch.Tensor,
+                  stream=None) -> None:
+    """tokens int32 [n_rows], the tree that the walk scored; result its sb_step_result."""
+    _need(tokens, 4, "tokens", torch.int32)
+    _need(result, STEP_RESULT_INTS * 4, "result", torch.int32)
+    _need(counts, 4, "counts", torch.int32)
+    _on_stream_device(stream, tokens, result, counts)
+    _check(lib.sb_count_step(counts.numel(), tokens.numel(), tokens.data_ptr(), result.data_ptr(),
+                             counts.data_ptr(), _stream(stream)), "sb_count_step")
+
+
+class LogitRules:
+    """An sb_logit_rules and the tensors it points to: prompt and output int32
+    [vocab] counts; bias float32 [vocab]; mask int32 or uint32 [ceil(vocab / 32)] or
+    [1][..] for all rows, [n_rows][..] for a mask per row.  All optional; the
+    tensors may change between calls, their shapes may not."""
+
+    def __init__(self, prompt=None, output=None, repetition: float = 1.0, presence: float = 0.0,
+                 frequency: float = 0.0, bias=None, mask=None):
+        self.tensors = (prompt, output, bias, mask)
+        for t, dt, name in ((prompt, torch.int32, "prompt"), (output, torch.int32, "output"),
+                            (bias, torch.float32, "bias")):
+            if t is not None:
+                _need(t, 0, name, dt)
+        if mask is not None:
+            if mask.dtype not in (torch.int32, torch.uint32) or mask.dim() not in (1, 2):
+                raise ValueError("mask: expected an int32 or uint32 tensor [words] or [rows][words]")
+            _need(mask, 0, "mask")
+        rows = 1 if mask is None or mask.dim() == 1 else mask.shape[0]
+        self.struct = LogitRulesStruct(_ptr(prompt), _ptr(output), repetition, presence, frequency,
+                                       _ptr(bias), _ptr(mask), 0 if rows == 1 else mask.shape[1])
+
+    def _check(self, vocab: int, n_rows: int) -> None:
+        for t, name in zip(self.tensors[:3], ("prompt", "output", "bias")):
+            if t is not None and t.numel() != vocab:
+                raise ValueError(f"{name}: {t.numel()} entries for a vocabulary of {vocab}")
+        mask = self.tensors[3]
+        if mask is None:
+            return
+        if mask.shape[-1] < (vocab + 31) // 32:
+            raise ValueError(f"mask: {mask.shape[-1]} words for a vocabulary of {vocab}")
+        if mask.dim() == 2 and mask.shape[0] not in (1, n_rows):
+            raise ValueError(f"mask: {mask.shape[0]} rows for a tree of {n_rows}")
+
+
+def sb_shape_workspace_bytes(vocab: int, n_rows: int) -> int:
+    return int(lib.sb_shape_workspace_bytes(vocab, n_rows))
+
+
+def sb_shape_logits(rules: LogitRules, tokens: torch.Tensor, parents, logits: torch.Tensor,
+                    out: torch.Tensor, temperature: float, stats: torch.Tensor, ws: torch.Tensor,
+                    stream=None) -> None:
+    """logits and out float32 [n_rows][vocab] (may be one tensor); tokens int32 [n_rows]."""
+    par, pp = _host_i32(parents)
+    n, v = len(par), logits.shape[-1]
+    _need(tokens, n * 4, "tokens", torch.int32)
+    _need(logits, n * v * 4, "logits", torch.float32)
+    if out.shape[-1] != v:
+        raise ValueError("out: another vocabulary than logits")
+    _need(out, n * v * 4, "out", torch.float32)
+    _need(stats, n * 16, "stats")
+    _need(ws, 0, "ws")
+    rules._check(v, n)
+    _on_stream_device(stream, tokens, logits, out, stats, ws, *rules.tensors)
+    _check(lib.sb_shape_logits(v, n, C.byref(rules.struct), tokens.data_ptr(), pp,
+                               logits.data_ptr(), out.data_ptr(), temperature, stats.data_ptr(),
+                               ws.data_ptr(), ws.nbytes, _stream(stream)), "sb_shape_logits")
 
 
 def sb_sample_workspace_bytes(vocab: int) -> int:

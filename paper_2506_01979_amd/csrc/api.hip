@@ -1610,4 +1610,70 @@ sb_status sb_verify_forward_quantized(sb_model *m, const sb_quantized_kv *kv, in
                       d_stats, (char *)d_ws, L, stream, &quant);
 }
 
+// ---- logits under penalties, biases and masks ----------------------------------
+
+sb_status sb_count_tokens(int32_t vocab, int32_t n, const int32_t *d_tokens, int32_t accumulate,
+                          int32_t *d_counts, hipStream_t stream) {
+  if (vocab < 1 || vocab > SB_BRANCH_MAX_VOCAB || n < 0 || (n > 0 && !d_tokens) || !d_counts)
+    return SB_ERR_INVALID_ARG;
+  if (n == 0 && accumulate) return SB_OK;
+  return hip_status(launch_count_tokens(vocab, n, d_tokens, accumulate != 0, d_counts, stream));
+}
+
+sb_status sb_count_step(int32_t vocab, int32_t n_rows, const int32_t *d_tokens,
+                        const sb_step_result *d_result, int32_t *d_counts, hipStream_t stream) {
+  if (vocab < 1 || vocab > SB_BRANCH_MAX_VOCAB || n_rows < 1 || n_rows > SB_MAX_ROWS || !d_tokens ||
+      !d_result || !d_counts)
+    return SB_ERR_INVALID_ARG;
+  return hip_status(launch_count_step(vocab, n_rows, d_tokens, d_result, d_counts, stream));
+}
+
+size_t sb_shape_workspace_bytes(int32_t vocab, int32_t n_rows) {
+  if (vocab < 1 || vocab > SB_BRANCH_MAX_VOCAB || n_rows < 1 || n_rows > SB_MAX_ROWS) return 0;
+  // every smaller tree may take the finer slices of few rows
+  const size_t here = (size_t)shape_groups(vocab, n_rows) * n_rows;
+  const size_t fewer = shape_groups(vocab, 1) == shape_groups(vocab, n_rows) ? here : 1024;
+  return align_up((here > fewer ? here : fewer) * sizeof(LmPart));
+}
+
+sb_status sb_shape_logits(int32_t vocab, int32_t n_rows, const sb_logit_rules *rules,
+                          const int32_t *d_tokens, const int32_t *h_parents, const float *d_logits,
+                          float *d_out, float temperature, sb_row_stats *d_stats, void *d_ws,
+                          size_t ws_bytes, hipStream_t stream) {
+  if (vocab < 1 || vocab > SB_BRANCH_MAX_VOCAB || !rules || !d_tokens || !d_logits || !d_out ||
+      !d_stats || !d_ws || !temperature_ok(temperature))
+    return SB_ERR_INVALID_ARG;
+  const sb_logit_rules &r = *rules;
+  if (!(r.repetition > 0.0f) || !isfinite(r.repetition) || !isfinite(r.presence) ||
+      !isfinite(r.frequency))
+    return SB_ERR_INVALID_ARG;
+  if (r.d_mask && r.mask_stride != 0 && r.mask_stride < (vocab + 31) / 32) return SB_ERR_INVALID_ARG;
+  TreeArg tree;
+  const sb_status st = check_tree(h_parents, n_rows, &tree);
+  if (st != SB_OK) return st;
+  if (ws_bytes < sb_shape_workspace_bytes(vocab, n_rows)) return SB_ERR_CAPACITY;
+  // what no rule needs is not read
+  const bool rep = r.repetition != 1.0f, pen = rep || r.presence != 0.0f || r.frequency != 0.0f;
+  ShapeArgs a{};
+  a.vocab = vocab;
+  a.logits = d_logits;
+  a.out = d_out;
+  a.prompt = rep ? r.d_prompt : nullptr;
+  a.output = pen ? r.d_output : nullptr;
+  a.bias = r.d_bias;
+  a.mask = r.d_mask;
+  a.mask_stride = r.mask_stride;
+  a.repetition = r.repetition;
+  a.presence = r.presence;
+  a.frequency = r.frequency;
+  a.tokens = d_tokens;
+  a.count_drafts = pen && n_rows > 1;
+  a.greedy = temperature <= 0.0f ? 1 : 0;
+  a.inv_t = a.greedy ? 1.0f : 1.0f / temperature;
+  a.part = (LmPart *)d_ws;
+  SB_TRY(launch_shape_logits(a, tree, n_rows, stream));
+  return hip_status(launch_stats_finish(a.part, shape_groups(vocab, n_rows), n_rows, temperature,
+                                        d_stats, stream, true));
+}
+
 }  // extern "C"

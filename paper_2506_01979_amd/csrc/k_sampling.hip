@@ -166,9 +166,11 @@ __global__ __launch_bounds__(1024) void k_softmax_stats_reg(const float *__restr
 // over the groups, zmax = fl32(lmax / T) (rounding is monotone, so this is
 // the largest scaled logit), and total = the float64 sum over groups of
 // sum_g exp(m_g - zmax), m_g = fl32(lmax_g / T), in a fixed order.  A row
-// with nothing above -inf has a NaN total at T > 0, as exp(-inf - -inf).
+// with nothing above -inf has a NaN total at T > 0, as exp(-inf - -inf), and
+// with `masked` at T = 0 too.
 __global__ __launch_bounds__(256) void k_softmax_stats_finish(const LmPart *__restrict__ part,
                                                              int groups, float inv_t, int greedy,
+                                                             int masked,
                                                              sb_row_stats *__restrict__ out) {
   constexpr int NW = 256 / 64;
   __shared__ float sbest[NW];
@@ -208,7 +210,7 @@ __global__ __launch_bounds__(256) void k_softmax_stats_finish(const LmPart *__re
     st.zmax = zmax;
     st.argmax = arg == INT_MAX ? 0 : arg;
     if (greedy)
-      st.total = isnan(s) ? (double)NAN : 1.0;
+      st.total = isnan(s) || (masked && best == -INFINITY) ? (double)NAN : 1.0;
     else
       st.total = best == -INFINITY ? (double)NAN : s;
     out[blockIdx.x] = st;
@@ -594,13 +596,13 @@ hipError_t launch_softmax_stats(int vocab, int n_rows, const float *logits, floa
 }
 
 hipError_t launch_stats_finish(const LmPart *part, int groups, int n_rows, float temperature,
-                               sb_row_stats *stats, hipStream_t s) {
+                               sb_row_stats *stats, hipStream_t s, bool masked) {
   if (groups < 1 || groups > 256 || n_rows < 1) return hipErrorInvalidValue;
   float inv_t;
   int greedy;
   temp_args(temperature, &inv_t, &greedy);
   hipLaunchKernelGGL(k_softmax_stats_finish, dim3(n_rows), dim3(256), 0, s, part, groups, inv_t,
-                     greedy, stats);
+                     greedy, masked ? 1 : 0, stats);
   return hipGetLastError();
 }
 

@@ -31,9 +31,32 @@ struct LmPart {
   double sum;
 };
 // One row per workgroup: the statistics of rows 0 .. n_rows - 1 from their
-// groups' partials, part[row][groups] (at most 256 groups).
+// groups' partials, part[row][groups] (at most 256 groups).  masked: a row
+// with nothing above -inf has NaN total at T = 0 too.
 hipError_t launch_stats_finish(const LmPart *part, int groups, int n_rows, float temperature,
-                               sb_row_stats *stats, hipStream_t s);
+                               sb_row_stats *stats, hipStream_t s, bool masked = false);
+// ---- counts and rules on logits (k_logits.hip) ------------------------------
+struct ShapeArgs {
+  int vocab;
+  const float *logits;
+  float *out;
+  const int32_t *prompt, *output;  // nullable, as below
+  const float *bias;
+  const uint32_t *mask;
+  int mask_stride;
+  float repetition, presence, frequency;
+  const int32_t *tokens;
+  int count_drafts;  // the drafts on a row's path count
+  float inv_t;
+  int greedy;
+  LmPart *part;  // [n_rows][shape_groups]
+};
+int shape_groups(int vocab, int n_rows);
+hipError_t launch_shape_logits(const ShapeArgs &a, const TreeArg &tree, int n_rows, hipStream_t s);
+hipError_t launch_count_tokens(int vocab, int n, const int32_t *tokens, int accumulate,
+                               int32_t *counts, hipStream_t s);
+hipError_t launch_count_step(int vocab, int n_rows, const int32_t *tokens,
+                             const sb_step_result *res, int32_t *counts, hipStream_t s);
 // How long a workgroup of the walk waits for the others' messages: ticks of the
 // 100 MHz s_memrealtime counter.  They arrive within microseconds unless other
 // work keeps some workgroups off the chip; that work may itself wait for the
