@@ -62,11 +62,17 @@ typedef enum {
   SB_ERR_UNSUPPORTED = 6    /* shape outside what the kernels handle */
 } sb_status;
 
-typedef enum { SB_F32 = 0, SB_BF16 = 1 } sb_dtype;
+typedef enum { SB_F32 = 0, SB_BF16 = 1, SB_INT8 = 2 } sb_dtype;
 
 /* Decoder shape (the paper's Table 7 lists the Llama widths).  SB_BF16
  * models store weights and KV in bfloat16 and accumulate in float32;
- * SB_F32 models are float32 throughout.  rope_theta is the RoPE base,
+ * SB_F32 models are float32 throughout.  SB_INT8 models hold the projections
+ * and the LM head in 8-bit integers with a scale per output channel and
+ * multiply them with activations quantised per token (the product of
+ * sb_linear_quantized; hidden, n_heads * head_dim and ffn at most
+ * SB_LINEAR_MAX_K); their embedding and KV cache are those of an SB_BF16
+ * model, and every call takes them where it takes one, but for the
+ * persistent forward.  rope_theta is the RoPE base,
  * rms_eps the RMSNorm epsilon. */
 typedef struct {
   int32_t n_layers, hidden, n_heads, n_kv_heads, head_dim, ffn, vocab;
@@ -75,7 +81,8 @@ typedef struct {
 } sb_model_config;
 
 /* Weight kinds for sb_pack_weight.  Sources are row-major [out][in]
- * matrices in the model dtype, as a Llama checkpoint stores them. */
+ * matrices in the model dtype (bfloat16 for SB_INT8), as a Llama checkpoint
+ * stores them. */
 typedef enum {
   SB_W_QKV = 0,     /* src0 = Wq [n_heads*head_dim][hidden], src1 = Wk, src2 = Wv
                        ([n_kv_heads*head_dim][hidden]) */
@@ -97,13 +104,13 @@ typedef struct {
 } sb_layer_weights;
 
 typedef struct {
-  const void *embed;               /* [vocab][hidden], model dtype, row-major */
+  const void *embed;               /* [vocab][hidden], model dtype (SB_INT8: bfloat16), row-major */
   const float *final_norm;         /* [hidden] */
   const void *lm_head;             /* packed SB_W_LM_HEAD */
   const sb_layer_weights *layers;  /* host array of n_layers entries */
 } sb_model_weights;
 
-/* KV cache in the model dtype: k is [n_layers][n_kv_heads][capacity][head_dim]
+/* KV cache in the model dtype (SB_INT8: bfloat16): k is [n_layers][n_kv_heads][capacity][head_dim]
  * (one key per row) and v is stored transposed, [n_layers][n_kv_heads]
  * [head_dim][capacity] (one value dimension per row), so attention reads both
  * with unit-stride vector loads along its own contraction.  capacity must be
@@ -175,7 +182,8 @@ size_t sb_packed_bytes(const sb_model_config *cfg, int32_t kind);
  * instruction (rows padded to 16 and columns to a multiple of 256 -- whole
  * chunks of 8 k-steps -- with zeros; Q/K rows of
  * every head reordered so a tile holds RoPE pairs (j, j + d/2); gate and up
- * rows interleaved 8 by 8); for SB_F32, the source rows concatenated
+ * rows interleaved 8 by 8); for SB_INT8, sb_linear_pack's form of the source
+ * rows concatenated; for SB_F32, the source rows concatenated
  * (Wq;Wk;Wv and Wgate;Wup).  src* and dst are device pointers, dst holds
  * sb_packed_bytes(cfg, kind) bytes and must not alias a source. */
 sb_status sb_pack_weight(const sb_model_config *cfg, int32_t kind, const void *src0,
@@ -285,7 +293,7 @@ sb_status sb_accept_resample(int32_t vocab, int32_t n_rows, const int32_t *d_tok
                              size_t ws_bytes, hipStream_t stream);
 
 /* How sb_verify_forward runs a bf16 model (the results are the same to the
- * bf16 tolerance; float32 models always use the kernel chain):
+ * bf16 tolerance; float32 and int8 models always use the kernel chain):
  *   SB_FWD_AUTO        the chain of kernels (the faster form on MI355X);
  *   SB_FWD_KERNELS     a chain of kernels, several per layer;
  *   SB_FWD_PERSISTENT  the persistent forward: every layer and the LM head
@@ -326,8 +334,8 @@ sb_status sb_kv_rollback(const sb_model *m, const sb_kv_cache *kv, int32_t kv_le
  * a call with more rows returns SB_ERR_CAPACITY): for k < k_layers - 1 the
  * residual stream after that layer, for the last one the final RMSNorm's
  * output RMSNorm(h) * g_final (the last hidden state in the form a library
- * Llama model reports it).  d_taps = NULL clears the tap.  SB_BF16 models
- * only (SB_ERR_DTYPE otherwise); 1 <= k_layers <= n_layers.  While a tap is
+ * Llama model reports it).  d_taps = NULL clears the tap.  Not for SB_F32
+ * models (SB_ERR_DTYPE); 1 <= k_layers <= n_layers.  While a tap is
  * set the forward runs as the chain of kernels (SB_FWD_KERNELS). */
 sb_status sb_model_set_tap(sb_model *m, float *d_taps, int32_t k_layers, int32_t max_rows);
 
@@ -590,6 +598,39 @@ sb_status sb_spec_round(sb_model *target, const sb_kv_cache *t_kv, int32_t t_len
                         int32_t *h_branches, void *d_ws, size_t ws_bytes,
                         hipStream_t verify_stream, hipStream_t draft_stream);
 
+/* ---- projections in 8-bit integers -------------------------------------- */
+
+/* Most inputs of a projection. */
+#define SB_LINEAR_MAX_K 32768
+
+/* Bytes of a packed weight matrix of m outputs and k inputs (0 for m < 1, m >
+ * 2^24, k < 1 or k > SB_LINEAR_MAX_K). */
+size_t sb_linear_packed_bytes(int32_t m, int32_t k);
+
+/* Quantises a bfloat16 matrix [m][k], row-major, per output: scale =
+ * fl32(amax / 127), code = nearest(127 w / amax), ties to even, amax the
+ * largest magnitude of the row (0 gives scale 0, a NaN or infinity in it a NaN
+ * scale), and lays the codes out in the operand order of the integer matrix
+ * instruction.  d_packed: sb_linear_packed_bytes(m, k) bytes, 16-byte
+ * aligned, not overlapping d_w. */
+sb_status sb_linear_pack(int32_t m, int32_t k, const void *d_w, void *d_packed,
+                         hipStream_t stream);
+
+/* Workspace bytes of sb_linear_quantized for up to max_rows rows (0 for
+ * arguments it rejects). */
+size_t sb_linear_workspace_bytes(int32_t m, int32_t k, int32_t max_rows);
+
+/* y = x W^T in 8-bit integers: every row of x gets codes nearest(127 x / amax)
+ * and a scale fl32(amax / 127) as the rows of W have, the codes are multiplied
+ * and summed exactly in 32-bit integers, and y[t][r] = float32(sum) *
+ * (scale_t * scale_r).  For an SB_F32 x, 127 x is rounded before the division.
+ *   d_packed: as sb_linear_pack writes it;
+ *   d_x: [n_rows][k], x_dtype SB_BF16 or SB_F32;  d_y: float32 [n_rows][m];
+ *   1 <= n_rows <= SB_MAX_ROWS. */
+sb_status sb_linear_quantized(int32_t m, int32_t k, const void *d_packed, int32_t n_rows,
+                              const void *d_x, int32_t x_dtype, float *d_y, void *d_ws,
+                              size_t ws_bytes, hipStream_t stream);
+
 /* ---- the prefix cache in 8 bits --------------------------------------- */
 
 /* Tokens that share one scale (per layer, KV head, and K or V). */
@@ -632,7 +673,7 @@ typedef struct {
 /* Quantises slots src_slot .. src_slot + 64 n_blocks - 1 of the bfloat16
  * cache src into blocks block .. block + n_blocks - 1 of dst, every layer and
  * KV head.  src_slot is a multiple of 8.  Of cfg, n_layers, n_kv_heads and
- * head_dim count, and dtype, which must be SB_BF16 (SB_ERR_DTYPE); here and
+ * head_dim count, and dtype, SB_BF16 or SB_INT8 (SB_ERR_DTYPE); here and
  * below n_heads must be a multiple of n_kv_heads.  n_blocks = 0 does nothing.
  * src may be dst->tail; dst->tail is not touched. */
 sb_status sb_kv_quantize(const sb_model_config *cfg, const sb_kv_cache *src, int32_t src_slot,
@@ -684,7 +725,7 @@ size_t sb_quantized_workspace_bytes(const sb_model *m, int32_t max_rows, int32_t
 /* sb_verify_forward with such a cache as the prefix: row i's K/V go to tail
  * slot tail_len + i, its position is 64 n_blocks + tail_len + depth(i).
  * Then sb_accept_resample, sb_kv_rollback(m, &kv->tail, tail_len, ...) and
- * sb_kv_commit.  SB_BF16 models (SB_ERR_DTYPE otherwise), as the chain of
+ * sb_kv_commit.  SB_BF16 and SB_INT8 models (SB_ERR_DTYPE otherwise), as the chain of
  * kernels (SB_ERR_UNSUPPORTED with SB_FWD_PERSISTENT set); the H-RAD tap is
  * written as by sb_verify_forward. */
 sb_status sb_verify_forward_quantized(sb_model *m, const sb_quantized_kv *kv, int32_t n_blocks,

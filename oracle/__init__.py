@@ -23,6 +23,8 @@ MI355X path computes, written from the paper:
   the branch point when the chain is accepted, and both caches rolled back;
 * ``oracle.quantized`` -- the prefix cache in 8 bits with a scale per block of 64
   tokens, and the branch-masked attention over it;
+* ``oracle.int8``     -- projections in 8-bit integers with a scale per token and
+  output channel, and the forward on them;
 * ``oracle.shaping``  -- penalties, biases and masks on the logits of a tree;
 * ``oracle.hrad``     -- H-RAD's length predictor (Section "H-RAD"): the
   last K layers' hidden states and the new token's embedding through a
@@ -38,4 +40,4 @@ output distribution, closed forms printed in the paper, hand-worked golden
 cases).  Nothing here is "parity unpinned".
 """
 
-from . import tree, decoder, sampling, rollback, hrad, branching, drafting, spec_round, quantized, shaping  # noqa: F401
+from . import tree, decoder, sampling, rollback, hrad, branching, drafting, spec_round, quantized, shaping, int8  # noqa: F401

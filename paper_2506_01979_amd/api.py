@@ -19,7 +19,7 @@ if not os.path.exists(_LIB_PATH):
 lib = C.CDLL(_LIB_PATH)
 
 SB_MAX_ROWS = 256
-SB_F32, SB_BF16 = 0, 1
+SB_F32, SB_BF16, SB_INT8 = 0, 1, 2
 SB_W_QKV, SB_W_O, SB_W_GATE_UP, SB_W_DOWN, SB_W_LM_HEAD = range(5)
 SB_FLAG_NONFINITE, SB_FLAG_QZERO, SB_FLAG_ZERO_RESIDUAL = 1, 2, 4
 
@@ -38,7 +38,9 @@ EXPORTS = ("sb_status_string", "sb_version", "sb_packed_bytes", "sb_pack_weight"
            "sb_spec_round_workspace_bytes", "sb_spec_round",
            "sb_kv_quantize", "sb_kv_dequantize", "sb_kv_commit", "sb_attend_workspace_bytes",
            "sb_attend_quantized", "sb_quantized_workspace_bytes", "sb_verify_forward_quantized",
-           "sb_count_tokens", "sb_count_step", "sb_shape_workspace_bytes", "sb_shape_logits")
+           "sb_count_tokens", "sb_count_step", "sb_shape_workspace_bytes", "sb_shape_logits",
+           "sb_linear_packed_bytes", "sb_linear_pack", "sb_linear_workspace_bytes",
+           "sb_linear_quantized")
 SB_FWD_AUTO, SB_FWD_KERNELS, SB_FWD_PERSISTENT = 0, 1, 2
 
 SB_HRAD_H1, SB_HRAD_H2, SB_HRAD_CLASSES = 256, 64, 3
@@ -202,6 +204,14 @@ lib.sb_quantized_workspace_bytes.argtypes = [_vp, _i32, _i32, _i32]
 lib.sb_verify_forward_quantized.restype = _i32
 lib.sb_verify_forward_quantized.argtypes = [_vp, C.POINTER(QuantizedKVStruct), _i32, _i32, _vp,
                                             C.POINTER(_i32), _i32, _f, _vp, _vp, _vp, _sz, _vp]
+lib.sb_linear_packed_bytes.restype = _sz
+lib.sb_linear_packed_bytes.argtypes = [_i32, _i32]
+lib.sb_linear_pack.restype = _i32
+lib.sb_linear_pack.argtypes = [_i32, _i32, _vp, _vp, _vp]
+lib.sb_linear_workspace_bytes.restype = _sz
+lib.sb_linear_workspace_bytes.argtypes = [_i32, _i32, _i32]
+lib.sb_linear_quantized.restype = _i32
+lib.sb_linear_quantized.argtypes = [_i32, _i32, _vp, _i32, _vp, _i32, _vp, _vp, _sz, _vp]
 lib.sb_count_tokens.restype = _i32
 lib.sb_count_tokens.argtypes = [_i32, _i32, _vp, _i32, _vp, _vp]
 lib.sb_count_step.restype = _i32
@@ -264,7 +274,14 @@ def _on_stream_device(stream, *tensors) -> None:
             raise ValueError(f"a tensor is on {t.device}, the current device is {cur}")
 
 
-def make_config(shape) -> ModelConfig:
+def make_config(shape, projections=None) -> ModelConfig:
+    """projections "int8": the SB_INT8 form of a bf16 shape."""
+    if projections not in (None, "int8") or (projections and shape.dtype != "bf16"):
+        raise ValueError("projections: None, or \"int8\" for a bf16 shape")
+    if projections:
+        return ModelConfig(shape.n_layers, shape.hidden, shape.n_heads, shape.n_kv_heads,
+                           shape.head_dim, shape.ffn, shape.vocab, shape.rope_theta, shape.rms_eps,
+                           SB_INT8)
     return ModelConfig(shape.n_layers, shape.hidden, shape.n_heads, shape.n_kv_heads,
                        shape.head_dim, shape.ffn, shape.vocab, shape.rope_theta, shape.rms_eps,
                        SB_BF16 if shape.dtype == "bf16" else SB_F32)
@@ -568,6 +585,48 @@ def sb_attend_quantized(cfg: ModelConfig, cache: QuantizedKV, layer: int, n_bloc
            "sb_attend_quantized")
 
 
+def sb_linear_packed_bytes(m: int, k: int) -> int:
+    return int(lib.sb_linear_packed_bytes(m, k))
+
+
+def sb_linear_pack(w: torch.Tensor, packed: torch.Tensor, stream=None) -> None:
+    """w bfloat16 [m][k]; packed of sb_linear_packed_bytes(m, k)."""
+    m, k = w.shape
+    _need(w, 0, "w", torch.bfloat16)
+    _need(packed, sb_linear_packed_bytes(m, k), "packed")
+    _on_stream_device(stream, w, packed)
+    _check(lib.sb_linear_pack(m, k, w.data_ptr(), packed.data_ptr(), _stream(stream)),
+           "sb_linear_pack")
+
+
+def sb_linear_workspace_bytes(m: int, k: int, max_rows: int) -> int:
+    return int(lib.sb_linear_workspace_bytes(m, k, max_rows))
+
+
+def sb_linear_quantized(packed: torch.Tensor, x: torch.Tensor, y: torch.Tensor, ws: torch.Tensor,
+                        stream=None) -> None:
+    """x bfloat16 or float32 [n][k]; y float32 [n][m]; packed as sb_linear_pack wrote it for
+    [m][k]; ws of sb_linear_workspace_bytes(m, k, n)."""
+    n, k = x.shape
+    m = y.shape[1]
+    if y.shape[0] != n:
+        raise ValueError(f"y: {y.shape[0]} rows for {n} of x")
+    if x.dtype not in (torch.bfloat16, torch.float32):
+        raise ValueError(f"x: expected bfloat16 or float32, got {x.dtype}")
+    _need(x, 0, "x")
+    _need(y, 0, "y", torch.float32)
+    need = sb_linear_packed_bytes(m, k)
+    if packed.nbytes != need:
+        raise ValueError(f"packed: {packed.nbytes} bytes, a [{m}][{k}] matrix has {need}")
+    _need(packed, need, "packed")
+    _need(ws, 0, "ws")
+    _on_stream_device(stream, packed, x, y, ws)
+    _check(lib.sb_linear_quantized(m, k, packed.data_ptr(), n, x.data_ptr(),
+                                   SB_BF16 if x.dtype is torch.bfloat16 else SB_F32, y.data_ptr(),
+                                   ws.data_ptr(), ws.nbytes, _stream(stream)),
+           "sb_linear_quantized")
+
+
 def sb_count_tokens(tokens: torch.Tensor, counts: torch.Tensor, accumulate: bool = True,
                     stream=None) -> None:
     """tokens int32 [n]; counts int32 [vocab]."""
@@ -699,12 +758,13 @@ class Model:
     or uint16 bfloat16 bit patterns); names are ``embed``, ``lm_head``,
     ``final_norm`` and per layer ``wq wk wv wo wg wu wd attn_norm mlp_norm``.
     Tensors are uploaded one at a time and packed with ``sb_pack_weight``;
-    the unpacked sources are freed once packed.
+    the unpacked sources are freed once packed.  ``projections="int8"``
+    packs a bf16 shape's projections and LM head in 8-bit integers (SB_INT8).
     """
 
-    def __init__(self, shape, tensor_fn, device="cuda", stream=None):
+    def __init__(self, shape, tensor_fn, device="cuda", stream=None, projections=None):
         self.shape = shape
-        self.cfg = make_config(shape)
+        self.cfg = make_config(shape, projections)
         self.device = device
         self.bf16 = shape.dtype == "bf16"
         self.wdtype = torch.bfloat16 if self.bf16 else torch.float32

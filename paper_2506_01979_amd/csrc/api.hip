@@ -56,6 +56,8 @@ struct Layout {
   size_t xa, act, q, part_o, part_ml, xn, ss, rs, pk_table, pk_sync;
   // f32
   size_t fq, fo, fact;
+  // int8: a projection's output, the codes and scales of its input
+  size_t y, xq, xs, ao;
   // attention over a quantised cache: partials of both its parts
   size_t quant_o, quant_ml;
   size_t total;
@@ -92,8 +94,9 @@ Layout make_layout(const sb_model_config &c, int n_rows, int kv_len, bool up_to 
   L.meta = take(sizeof(Meta));
   L.rope = take((size_t)np * (d / 2) * sizeof(float2));
   L.h = take((size_t)np * H * sizeof(float));
-  if (c.dtype == SB_BF16) {
-    L.delta = take((size_t)kMaxSplit * np * H * sizeof(float));
+  if (c.dtype != SB_F32) {
+    const bool int8 = c.dtype == SB_INT8;
+    L.delta = take((size_t)(int8 ? 1 : kMaxSplit) * np * H * sizeof(float));
     // packed activations use the k-steps of the weights they multiply
     L.ks_h = pack_geom(c, SB_W_QKV).ks;
     L.ks_o = pack_geom(c, SB_W_O).ks;
@@ -112,6 +115,19 @@ Layout make_layout(const sb_model_config &c, int n_rows, int kv_len, bool up_to 
     part_rows(n_rows * G);
     if (up_to && n_rows * G > 16 * kAttnMaxRowTiles) part_rows(16 * kAttnMaxRowTiles / G * G);
     for (int r = 16 * kAttnMaxWaves; up_to && r < n_rows * G; r += 16 * kAttnMaxWaves) part_rows(r / G * G);
+    L.q = take((size_t)np * qd * 2);
+    L.part_o = take(c.n_kv_heads * parts * d * sizeof(float));
+    L.part_ml = take(c.n_kv_heads * parts * 2 * sizeof(float));
+    if (int8) {
+      const int most = ksx > L.ks_f ? ksx : L.ks_f;
+      const int wide = qd + 2 * c.n_kv_heads * d;
+      L.y = take((size_t)np * (wide > 2 * F ? wide : 2 * F) * sizeof(float));
+      L.xq = take((size_t)np * most * 64);
+      L.xs = take((size_t)np * sizeof(float));
+      L.ao = take((size_t)np * qd * 2);
+      L.total = off;
+      return L;
+    }
     L.xa = take((size_t)np * ksx * 32 * 2);
     L.act = take((size_t)np * L.ks_f * 32 * 2);
     // the post-attention RMSNorm fused into the O projection: gated
@@ -120,9 +136,6 @@ Layout make_layout(const sb_model_config &c, int n_rows, int kv_len, bool up_to 
     L.ss = take((size_t)np * kSsGroups * sizeof(float));
     // 1/rms per row of the last RMSNorm kernel (its projection's scale)
     L.rs = take((size_t)np * sizeof(float));
-    L.q = take((size_t)np * qd * 2);
-    L.part_o = take(c.n_kv_heads * parts * d * sizeof(float));
-    L.part_ml = take(c.n_kv_heads * parts * 2 * sizeof(float));
     // the persistent kernel's layer table and barrier counters
     L.pk_table = take((size_t)c.n_layers * sizeof(PkLayer));
     L.pk_sync = take(sizeof(PkSync));
@@ -143,14 +156,17 @@ bool config_ok(const sb_model_config *c) {
   if (c->n_heads % c->n_kv_heads != 0) return false;
   if (c->head_dim % 16 != 0) return false;
   if (!(c->rms_eps > 0.0f) || !(c->rope_theta > 0.0f)) return false;
-  if (c->dtype != SB_F32 && c->dtype != SB_BF16) return false;
+  if (c->dtype != SB_F32 && c->dtype != SB_BF16 && c->dtype != SB_INT8) return false;
   return true;
 }
 
 sb_status shape_supported(const sb_model_config *c) {
-  if (c->dtype == SB_BF16) {
+  if (c->dtype != SB_F32) {
     if (c->head_dim != 64 && c->head_dim != 128) return SB_ERR_UNSUPPORTED;
     if (c->hidden % 8 != 0 || c->hidden > 16384) return SB_ERR_UNSUPPORTED;
+    if (c->dtype == SB_INT8 && (c->ffn > kLinearMaxK ||
+                                (int64_t)c->n_heads * c->head_dim > kLinearMaxK))
+      return SB_ERR_UNSUPPORTED;
   } else {
     if (c->head_dim > 256) return SB_ERR_UNSUPPORTED;
   }
@@ -180,7 +196,8 @@ inline sb_status hip_status(hipError_t e) { return e == hipSuccess ? SB_OK : SB_
     if (_e != hipSuccess) return SB_ERR_HIP;      \
   } while (0)
 
-size_t elem_bytes(const sb_model_config &c) { return c.dtype == SB_BF16 ? 2 : 4; }
+// Bytes of a cached value or an embedding entry.
+size_t elem_bytes(const sb_model_config &c) { return c.dtype == SB_F32 ? 4 : 2; }
 
 // Embedding / metadata arguments.
 EmbedArgs embed_args(const sb_model *m, const int32_t *tokens, float *h, int n, int kv_len,
@@ -201,7 +218,7 @@ EmbedArgs embed_args(const sb_model *m, const int32_t *tokens, float *h, int n, 
   return ea;
 }
 
-// Times one launch of kernel class kc with the model's timer events: a GEMM
+// Times one launch of kernel class kc with the model's timer events: a bf16 GEMM
 // class hands them to its dispatch (which records the kernel's own start and
 // end), any other class records them before and after its launch.
 struct TimedLaunch {
@@ -211,8 +228,9 @@ struct TimedLaunch {
   TimedLaunch(sb_model *m, int kc, hipStream_t st)
       : t(m->timer), s(st), on(m->timer.active && m->timer.kernel_class == kc &&
                                m->timer.used < (int)m->timer.start.size()),
-        gemm(kc == SB_KC_QKV || kc == SB_KC_O || kc == SB_KC_GATE_UP || kc == SB_KC_DOWN ||
-             kc == SB_KC_LM_HEAD) {
+        gemm(m->cfg.dtype == SB_BF16 &&
+             (kc == SB_KC_QKV || kc == SB_KC_O || kc == SB_KC_GATE_UP || kc == SB_KC_DOWN ||
+              kc == SB_KC_LM_HEAD)) {
     if (!on) return;
     if (gemm)
       g_launch_events = LaunchEvents{t.start[t.used], t.stop[t.used], false};
@@ -474,6 +492,103 @@ sb_status forward_bf16(sb_model *m, const sb_kv_cache *kv, int kv_len, const int
   return SB_OK;
 }
 
+// The forward of an int8 model, as a chain of kernels: every projection reads
+// codes and scales that the launch before it left (xq, xs).  quant as in
+// forward_bf16.
+sb_status forward_int8(sb_model *m, const sb_kv_cache *kv, int kv_len, const int32_t *tokens,
+                       const TreeArg &tree, int n, float temperature, float *logits,
+                       sb_row_stats *stats, char *ws, const Layout &L, hipStream_t s,
+                       const QuantPrefix *quant = nullptr) {
+  const sb_model_config &c = m->cfg;
+  const int H = c.hidden, d = c.head_dim, F = c.ffn, qd = c.n_heads * d;
+  Meta *meta = (Meta *)(ws + L.meta);
+  float2 *rope = (float2 *)(ws + L.rope);
+  float *h = (float *)(ws + L.h), *delta = (float *)(ws + L.delta), *y = (float *)(ws + L.y);
+  uint8_t *xq = (uint8_t *)(ws + L.xq);
+  float *xs = (float *)(ws + L.xs);
+  uint16_t *q = (uint16_t *)(ws + L.q), *ao = (uint16_t *)(ws + L.ao);
+
+  const int prefix = quant ? quant->n_blocks * SB_KV_BLOCK : 0;
+  SB_TRY(launch_embed_meta(embed_args(m, tokens, h, n, prefix + kv_len, meta, rope), tree, L.np, 1,
+                           s));
+  const size_t layer_kv = (size_t)c.n_kv_heads * kv->capacity * d;
+  auto tap_of = [&](int li) -> float * {
+    const int idx = li - (c.n_layers - m->tap_k);
+    if (!m->tap || li < 0 || idx < 0) return nullptr;
+    return m->tap + (size_t)idx * m->tap_rows * H;
+  };
+  auto linear = [&](int kind, const void *w, float *out) {
+    const PackGeom g = pack_geom(c, kind);
+    LinearArgs a{};
+    a.w = (const uint8_t *)w;
+    a.w_scale = (const float *)(a.w + linear_geom(g.rows, g.K).scales);
+    a.x = xq;
+    a.x_scale = xs;
+    a.y = out;
+    a.m = g.rows;
+    a.tiles = g.tiles;
+    a.ks = g.ks;
+    a.n_tok = n;
+    return launch_linear(a, s);
+  };
+  RopeStoreArgs ra{};
+  ra.y = y;
+  ra.rope = rope;
+  ra.q = q;
+  ra.n_tok = n;
+  ra.n_heads = c.n_heads;
+  ra.n_kv = c.n_kv_heads;
+  ra.head_dim = d;
+  ra.cap = kv->capacity;
+  ra.kv_len = kv_len;
+  AttnArgs aa{};
+  aa.q = q;
+  aa.cap = kv->capacity;
+  aa.kv_len = kv_len;
+  aa.n_tok = n;
+  aa.n_heads = c.n_heads;
+  aa.n_kv = c.n_kv_heads;
+  aa.head_dim = d;
+  aa.n_chunks = L.n_chunks;
+  aa.meta = meta;
+  aa.scale = 1.0f / sqrtf((float)d);
+  aa.part_o = (float *)(ws + L.part_o);
+  aa.part_ml = (float *)(ws + L.part_ml);
+
+  for (int l = 0; l < c.n_layers; ++l) {
+    const sb_layer_weights &lw = m->layers[l];
+    SB_TIMED(SB_KC_NORM, launch_norm_quant(h, l ? delta : nullptr, lw.attn_norm, H, n, c.rms_eps, xq,
+                                           xs, s, tap_of(l - 1), 0));
+    SB_TIMED(SB_KC_QKV, linear(SB_W_QKV, lw.qkv, y));
+    ra.kc = (uint16_t *)kv->k + l * layer_kv;
+    ra.vc = (uint16_t *)kv->v + l * layer_kv;
+    SB_TRY(launch_rope_store(ra, s));
+    if (quant) {
+      const QuantAttnArgs qa =
+          quant_attn_args(c, *quant->kv, l, quant->n_blocks, kv_len, n, q, meta, ws, L);
+      SB_TIMED(SB_KC_ATTN, launch_attn_quant(qa, s));
+      SB_TIMED(SB_KC_ATTN_MERGE, launch_attn_merge_bf16(quant_merge_args(qa), ao, 0, s));
+    } else {
+      aa.kc = ra.kc;
+      aa.vc = ra.vc;
+      SB_TIMED(SB_KC_ATTN, launch_attn_bf16(aa, s));
+      SB_TIMED(SB_KC_ATTN_MERGE, launch_attn_merge_bf16(aa, ao, 0, s));
+    }
+    SB_TRY(launch_quant_rows(ao, true, n, qd, xq, xs, s));
+    SB_TIMED(SB_KC_O, linear(SB_W_O, lw.o, delta));
+    SB_TIMED(SB_KC_NORM, launch_norm_quant(h, delta, lw.mlp_norm, H, n, c.rms_eps, xq, xs, s,
+                                           nullptr, 0));
+    SB_TIMED(SB_KC_GATE_UP, linear(SB_W_GATE_UP, lw.gate_up, y));
+    SB_TRY(launch_swiglu_quant(y, n, F, xq, xs, s));
+    SB_TIMED(SB_KC_DOWN, linear(SB_W_DOWN, lw.down, delta));
+  }
+  SB_TIMED(SB_KC_NORM, launch_norm_quant(h, delta, m->final_norm, H, n, c.rms_eps, xq, xs, s,
+                                         tap_of(c.n_layers - 1), 1));
+  SB_TIMED(SB_KC_LM_HEAD, linear(SB_W_LM_HEAD, m->lm_head, logits));
+  SB_TIMED(SB_KC_STATS, launch_softmax_stats(c.vocab, n, logits, temperature, stats, s));
+  return SB_OK;
+}
+
 // The persistent forward of a bf16 model: embedding and tree metadata, the
 // layer table, one cooperative launch for every layer and the LM head, then
 // the row statistics.
@@ -698,6 +813,20 @@ sb_status sb_pack_weight(const sb_model_config *cfg, int32_t kind, const void *s
     if (shape_supported(cfg) != SB_OK) return SB_ERR_UNSUPPORTED;
     return hip_status(launch_pack_bf16(kind, c, src0, src1, src2, dst, stream));
   }
+  if (c.dtype == SB_INT8) {
+    if (shape_supported(cfg) != SB_OK) return SB_ERR_UNSUPPORTED;
+    const int qd = c.n_heads * c.head_dim, kvd = c.n_kv_heads * c.head_dim;
+    LinearPackArgs a{};
+    a.src[0] = (const uint16_t *)src0;
+    a.src[1] = (const uint16_t *)src1;
+    a.src[2] = (const uint16_t *)src2;
+    a.rows[0] = kind == SB_W_QKV ? qd : kind == SB_W_GATE_UP ? c.ffn : pack_geom(c, kind).rows;
+    a.rows[1] = kind == SB_W_QKV ? kvd : kind == SB_W_GATE_UP ? c.ffn : 0;
+    a.rows[2] = kind == SB_W_QKV ? kvd : 0;
+    a.k = pack_geom(c, kind).K;
+    a.codes = (uint8_t *)dst;
+    return hip_status(launch_linear_pack(a, stream));
+  }
   // float32: concatenated row-major sources
   const size_t H = c.hidden, qd = (size_t)c.n_heads * c.head_dim,
                kvd = (size_t)c.n_kv_heads * c.head_dim, F = c.ffn;
@@ -829,7 +958,7 @@ sb_status sb_verify_forward(sb_model *m, const sb_kv_cache *kv, int32_t kv_len,
   sb_status st = check_tree(h_parents, n_rows, &tree);
   if (st != SB_OK) return st;
   if ((int64_t)kv_len + n_rows > kv->capacity || kv->capacity % 8 != 0) return SB_ERR_CAPACITY;
-  if (m->cfg.dtype == SB_BF16 && (int64_t)kv_len + n_rows > kBf16MaxKeys) return SB_ERR_UNSUPPORTED;
+  if (m->cfg.dtype != SB_F32 && (int64_t)kv_len + n_rows > kBf16MaxKeys) return SB_ERR_UNSUPPORTED;
   if (m->cfg.dtype == SB_F32 && kv_len + n_rows > kF32MaxKeys) return SB_ERR_UNSUPPORTED;
   const Layout L = make_layout(m->cfg, n_rows, kv_len);
   if (ws_bytes < L.total) return SB_ERR_CAPACITY;
@@ -851,6 +980,9 @@ sb_status sb_verify_forward(sb_model *m, const sb_kv_cache *kv, int32_t kv_len,
                         (char *)d_ws, L, stream);
   }
   if (m->fwd_mode == SB_FWD_PERSISTENT) return SB_ERR_UNSUPPORTED;
+  if (m->cfg.dtype == SB_INT8)
+    return forward_int8(m, kv, kv_len, d_tokens, tree, n_rows, temperature, d_logits, d_stats,
+                        (char *)d_ws, L, stream);
   return forward_f32(m, kv, kv_len, d_tokens, tree, n_rows, temperature, d_logits, d_stats,
                      (char *)d_ws, L, stream);
 }
@@ -970,7 +1102,7 @@ sb_status sb_model_set_tap(sb_model *m, float *d_taps, int32_t k_layers, int32_t
     m->tap_k = m->tap_rows = 0;
     return SB_OK;
   }
-  if (m->cfg.dtype != SB_BF16) return SB_ERR_DTYPE;
+  if (m->cfg.dtype == SB_F32) return SB_ERR_DTYPE;
   if (k_layers < 1 || k_layers > m->cfg.n_layers || max_rows < 1 || max_rows > SB_MAX_ROWS)
     return SB_ERR_INVALID_ARG;
   m->tap = d_taps;
@@ -988,7 +1120,7 @@ sb_status sb_hrad_predict(const sb_model *m, const float *d_taps, int32_t k_laye
   if (!m || !d_taps || !d_result || !w || !d_logits3 || !d_class || !d_ws)
     return SB_ERR_INVALID_ARG;
   if (!w->w1 || !w->b1 || !w->w2 || !w->b2 || !w->w3 || !w->b3) return SB_ERR_INVALID_ARG;
-  if (m->cfg.dtype != SB_BF16) return SB_ERR_DTYPE;
+  if (m->cfg.dtype == SB_F32) return SB_ERR_DTYPE;
   if (k_layers < 1 || k_layers > m->cfg.n_layers || max_rows < 1 || max_rows > SB_MAX_ROWS)
     return SB_ERR_INVALID_ARG;
   if (ws_bytes < sb_hrad_workspace_bytes()) return SB_ERR_CAPACITY;
@@ -1426,7 +1558,7 @@ static sb_status check_attention_config(const sb_model_config *c) {
   if (!c || c->n_layers <= 0 || c->n_heads <= 0 || c->n_kv_heads <= 0 ||
       c->n_heads % c->n_kv_heads != 0)
     return SB_ERR_INVALID_ARG;
-  if (c->dtype != SB_BF16) return SB_ERR_DTYPE;
+  if (c->dtype != SB_BF16 && c->dtype != SB_INT8) return SB_ERR_DTYPE;
   if (c->head_dim != 64 && c->head_dim != 128) return SB_ERR_UNSUPPORTED;
   // rows of query heads, and (layer, head, block) grids, in 32 bits
   if (c->n_heads > 4096 || (int64_t)c->n_layers * c->n_kv_heads > (1 << 16))
@@ -1606,6 +1738,9 @@ sb_status sb_verify_forward_quantized(sb_model *m, const sb_quantized_kv *kv, in
   if (m->tap && n_rows > m->tap_rows) return SB_ERR_CAPACITY;
   if (m->fwd_mode == SB_FWD_PERSISTENT) return SB_ERR_UNSUPPORTED;
   const QuantPrefix quant{kv, n_blocks};
+  if (m->cfg.dtype == SB_INT8)
+    return forward_int8(m, &kv->tail, tail_len, d_tokens, tree, n_rows, temperature, d_logits,
+                        d_stats, (char *)d_ws, L, stream, &quant);
   return forward_bf16(m, &kv->tail, tail_len, d_tokens, tree, n_rows, temperature, d_logits,
                       d_stats, (char *)d_ws, L, stream, &quant);
 }
@@ -1674,6 +1809,59 @@ sb_status sb_shape_logits(int32_t vocab, int32_t n_rows, const sb_logit_rules *r
   SB_TRY(launch_shape_logits(a, tree, n_rows, stream));
   return hip_status(launch_stats_finish(a.part, shape_groups(vocab, n_rows), n_rows, temperature,
                                         d_stats, stream, true));
+}
+
+// ---- projections in 8-bit integers ------------------------------------------------
+
+static bool linear_ok(int32_t m, int32_t k) {
+  return m >= 1 && m <= (1 << 24) && k >= 1 && k <= SB_LINEAR_MAX_K;
+}
+
+size_t sb_linear_packed_bytes(int32_t m, int32_t k) {
+  return linear_ok(m, k) ? linear_geom(m, k).bytes : 0;
+}
+
+sb_status sb_linear_pack(int32_t m, int32_t k, const void *d_w, void *d_packed,
+                         hipStream_t stream) {
+  if (!linear_ok(m, k) || !d_w || !d_packed || ((uintptr_t)d_packed & 15) != 0)
+    return SB_ERR_INVALID_ARG;
+  LinearPackArgs a{};
+  a.src[0] = (const uint16_t *)d_w;
+  a.rows[0] = m;
+  a.k = k;
+  a.codes = (uint8_t *)d_packed;
+  return hip_status(launch_linear_pack(a, stream));
+}
+
+size_t sb_linear_workspace_bytes(int32_t m, int32_t k, int32_t max_rows) {
+  if (!linear_ok(m, k) || max_rows < 1 || max_rows > SB_MAX_ROWS) return 0;
+  const size_t rows = round_up(max_rows, 16);
+  return align_up(rows * linear_geom(m, k).ks * 64) + align_up(rows * sizeof(float));
+}
+
+sb_status sb_linear_quantized(int32_t m, int32_t k, const void *d_packed, int32_t n_rows,
+                              const void *d_x, int32_t x_dtype, float *d_y, void *d_ws,
+                              size_t ws_bytes, hipStream_t stream) {
+  if (!linear_ok(m, k) || !d_packed || !d_x || !d_y || !d_ws || n_rows < 1 ||
+      n_rows > SB_MAX_ROWS || (((uintptr_t)d_packed | (uintptr_t)d_ws) & 15) != 0)
+    return SB_ERR_INVALID_ARG;
+  if (x_dtype != SB_BF16 && x_dtype != SB_F32) return SB_ERR_DTYPE;
+  if (ws_bytes < sb_linear_workspace_bytes(m, k, n_rows)) return SB_ERR_CAPACITY;
+  const LinearGeom g = linear_geom(m, k);
+  LinearArgs a{};
+  uint8_t *codes = (uint8_t *)d_ws;
+  float *scales = (float *)(codes + align_up((size_t)round_up(n_rows, 16) * g.ks * 64));
+  a.w = (const uint8_t *)d_packed;
+  a.w_scale = (const float *)(a.w + g.scales);
+  a.x = codes;
+  a.x_scale = scales;
+  a.y = d_y;
+  a.m = m;
+  a.tiles = g.tiles;
+  a.ks = g.ks;
+  a.n_tok = n_rows;
+  SB_TRY(launch_quant_rows(d_x, x_dtype == SB_BF16, n_rows, k, codes, scales, stream));
+  return hip_status(launch_linear(a, stream));
 }
 
 }  // extern "C"

@@ -28,11 +28,18 @@ struct PackGeom {
 inline int ceil_div(int a, int b) { return (a + b - 1) / b; }
 inline int round_up(int a, int b) { return ceil_div(a, b) * b; }
 
+// A packed weight matrix: codes [tiles][ks][64 lanes][16], then the scales
+// [tiles * 16] at byte `scales`.
+struct LinearGeom {
+  int tiles, ks;
+  size_t scales, bytes;
+};
+LinearGeom linear_geom(int m, int k);
+
 inline PackGeom pack_geom(const sb_model_config &c, int kind) {
   PackGeom g{};
   const int H = c.hidden, d = c.head_dim, F = c.ffn;
   const int qd = c.n_heads * d, kvd = c.n_kv_heads * d;
-  const bool bf = c.dtype == SB_BF16;
   switch (kind) {
     case SB_W_QKV:
       g.K = H;
@@ -62,7 +69,12 @@ inline PackGeom pack_geom(const sb_model_config &c, int kind) {
     default:
       return g;
   }
-  if (bf) {
+  if (c.dtype == SB_INT8) {
+    const LinearGeom l = linear_geom(g.rows, g.K);
+    g.ks = l.ks;
+    g.tiles = l.tiles;
+    g.bytes = l.bytes;
+  } else if (c.dtype == SB_BF16) {
     g.ks = round_up(ceil_div(g.K, 32), 8);  // whole 8-k-step chunks
     g.bytes = (size_t)g.tiles * g.ks * 1024;
   } else {
@@ -306,6 +318,54 @@ struct QuantAttnArgs {
 };
 hipError_t launch_tree_masks(Meta *meta, const TreeArg &tree, hipStream_t s);
 hipError_t launch_attn_quant(const QuantAttnArgs &a, hipStream_t s);
+
+// ---- 8-bit projections (k_linear.hip) ------------------------------------------
+// Most inputs of a projection (a row of it is held in registers), most token
+// tiles of a workgroup.
+constexpr int kLinearMaxK = SB_LINEAR_MAX_K;
+constexpr int kLinearMaxTokenTiles = 8;
+struct LinearPackArgs {
+  const uint16_t *src[3];  // bf16, stacked along the outputs
+  int rows[3];
+  int k;
+  uint8_t *codes;  // the packed matrix
+  int ks;          // filled in by the launch
+  float *scale;
+};
+hipError_t launch_linear_pack(const LinearPackArgs &a, hipStream_t s);
+// Rows x [n_tok][k] (bf16 or float32) to codes [round_up(n_tok, 16)][64 ks] and scales.
+hipError_t launch_quant_rows(const void *x, bool bf16, int n_tok, int k, uint8_t *codes,
+                             float *scale, hipStream_t s);
+struct LinearArgs {
+  const uint8_t *w;  // codes, in operand order
+  const float *w_scale;
+  const uint8_t *x;
+  const float *x_scale;
+  float *y;  // [n_tok][m]
+  int m, tiles, ks, n_tok;
+  int vec, ttiles, tblocks;  // filled in by the launch
+};
+hipError_t launch_linear(const LinearArgs &a, hipStream_t s);
+
+// What stands between the projections of an int8 model (k_int8.hip).
+// The residual rows h [n_tok][hidden], delta (nullable, [n_tok][hidden]) added and
+// stored back, their RMSNorm with gain g to codes and scales; tap and
+// tap_normed as launch_rmsnorm_pack.
+hipError_t launch_norm_quant(float *h, const float *delta, const float *g, int hidden, int n_tok,
+                             float eps, uint8_t *codes, float *scale, hipStream_t s, float *tap,
+                             int tap_normed);
+// y [n_tok][(n_heads + 2 n_kv) d] = q, k, v: RoPE on q and k, bf16 q to q, k and v to
+// the cache's slots kv_len + t.
+struct RopeStoreArgs {
+  const float *y;
+  const float2 *rope;
+  uint16_t *q, *kc, *vc;
+  int n_tok, n_heads, n_kv, head_dim, cap, kv_len;
+};
+hipError_t launch_rope_store(const RopeStoreArgs &a, hipStream_t s);
+// y [n_tok][2 ffn] = gate, up: silu(gate) up to codes and scales.
+hipError_t launch_swiglu_quant(const float *y, int n_tok, int ffn, uint8_t *codes, float *scale,
+                               hipStream_t s);
 
 // ---- persistent forward (k_persist.hip) ------------------------------------
 // One cooperative launch runs every layer of a bf16 verify forward: one
