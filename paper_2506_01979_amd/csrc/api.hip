@@ -254,13 +254,14 @@ struct TimedLaunch {
 // Partials of the attention over a quantised cache: room for every call of at
 // most n_rows rows, n_blocks blocks and tail_len tail slots (ranges x rows of a
 // KV head: quant_attn_plan's ranges are at most kQuantTargetGroups over the KV
-// heads and row blocks, or 2, and a range has four steps).
+// heads and row blocks, or 2, and one more, and a range has four steps).
 void take_quant_partials(const sb_model_config &c, int n_rows, int n_blocks, int tail_len,
                          Layout *L) {
   const int64_t rows = (int64_t)n_rows * (c.n_heads / c.n_kv_heads);
   const int64_t per_block = 16 * kQuantMaxRowTiles;
   int64_t parts = kQuantTargetGroups * (rows < per_block ? rows : per_block);
   if (parts < 2 * c.n_kv_heads * rows) parts = 2 * c.n_kv_heads * rows;
+  parts += c.n_kv_heads * rows;
   const int64_t ranges = ceil_div(n_blocks, 4) + ceil_div(ceil_div(tail_len + n_rows, 32), 4);
   if (parts > ranges * c.n_kv_heads * rows) parts = ranges * c.n_kv_heads * rows;
   L->quant_o = L->total;

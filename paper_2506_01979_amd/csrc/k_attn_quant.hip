@@ -17,14 +17,14 @@
 // 1024 and subtracting 1152, e4m3 by the conversion instruction.  The scales
 // never touch the codes: K's multiplies the scores with the softmax factor, V's
 // multiplies the softmax weights,
-//   S^T = K Q^T;  p = exp2(s kscale c - m);  l += p;  O^T += V^T (p r)^T,
+//   S^T = K Q^T;  w = exp2(s kscale c - m + log2 r);  l += w / r;  O^T += V^T w^T,
 //   r = vscale 2^15 / (the largest vscale of the wave's blocks),
-// so that p r <= 2^15 is binary16 to 11 bits down to 2^-29 of the largest
+// so that w <= 2^15 is binary16 to 11 bits down to 2^-29 of the largest
 // weight.  Those 11 bits are the products' rounding point: an eighth of what
 // the output's bfloat16 keeps, and one matrix instruction where the two parts
 // of k_attn.hip take two.  Q enters as binary16 scaled by a power of two per
 // row (largest magnitude in [2^14, 2^15)): exact for elements down to 2^-28 of it.
-// l sums the unrounded float32 p.
+// l sums the unrounded float32 w.
 //
 // A tail step (32 keys) is computed as in k_attn.hip: bfloat16 Q, K and V, the
 // weights in two bfloat16 parts, the tree mask on the scores.
@@ -75,6 +75,10 @@ __device__ __forceinline__ f16x8 widen8(uint32_t w0, uint32_t w1) {
   return __builtin_bit_cast(f16x8, o);
 }
 
+__device__ __forceinline__ float lane_value(float v, int lane) {
+  return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), lane));
+}
+
 // D: head_dim; RT: 16-row query tiles of the workgroup.
 template <int D, int FMT, int RT>
 __global__ __launch_bounds__(kT, 2) void k_attn_quant(QuantAttnArgs a) {
@@ -93,13 +97,42 @@ __global__ __launch_bounds__(kT, 2) void k_attn_quant(QuantAttnArgs a) {
   const int lr = lane & 15, lg = lane >> 4;
   const int G = a.n_heads / a.n_kv;
   const int R = a.n_tok * G;
-  // Work unit (KV head, range, row block), XCD-major, the row block fastest
-  // (the workgroups of one range share its reads through the L2).
-  const int xcd = blockIdx.x & 7, left = gridDim.x & 7;
-  const int unit = xcd * (gridDim.x >> 3) + (xcd < left ? xcd : left) + (blockIdx.x >> 3);
-  const int rb = unit % a.n_rb, g = unit / a.n_rb / a.n_chunks, split = unit / a.n_rb % a.n_chunks;
-  const bool quant = split < a.c8;
+  // Work unit (range, KV head, row block).  The row blocks of one range and head
+  // follow each other on one XCD (workgroup b runs on XCD b % 8) and share its
+  // reads through the L2; the tail's ranges, short ones, come first, so that what
+  // does not fit the chip at once fills up behind them.
+  const int turn = blockIdx.x >> 3;
+  const int rb = turn % a.n_rb, unit = turn / a.n_rb * 8 + (blockIdx.x & 7);
+  if (unit >= a.n_kv * a.n_chunks) return;
+  const int g = unit % a.n_kv, split = unit / a.n_kv;
+  const bool quant = split >= a.ct;
   const float c = a.scale * 1.44269504088896340736f;  // exp(x scale) = exp2(x c)
+
+  // ---- an 8-bit range's first loads go out before anything waits: the wave's
+  // first block, and the scales of its first 64 blocks, one per lane
+  const int b0 = quant ? (int)((int64_t)a.n_blocks * (split - a.ct) / a.c8) : 0;
+  const int b1 = quant ? (int)((int64_t)a.n_blocks * (split - a.ct + 1) / a.c8) : 0;
+  const float *ks = a.k_scale + (size_t)g * a.cap_blocks, *vs = a.v_scale + (size_t)g * a.cap_blocks;
+  const int bytes = a.cap_blocks * SB_KV_BLOCK * D;  // one head's codes: at most 2^27
+  const __amdgpu_buffer_rsrc_t krs = uniform_rsrc(a.k8 + (size_t)g * bytes, bytes);
+  const __amdgpu_buffer_rsrc_t vrs = uniform_rsrc(a.v8 + (size_t)g * bytes, bytes);
+  i32x4 kf[NF], vf[NF];
+  auto load = [&](i32x4 (&f)[NF], __amdgpu_buffer_rsrc_t rs, int b) {
+    const int vo = b < b1 ? b * (SB_KV_BLOCK * D) + lane * 16 : bytes;
+#pragma unroll
+    for (int i = 0; i < NF; ++i) f[i] = __builtin_amdgcn_raw_buffer_load_b128(rs, vo, i * 1024, 0);
+  };
+  float kscales = 0.0f, vscales = 0.0f;
+  auto load_scales = [&](int b) {
+    const bool in = b + kNW * lane < b1;
+    kscales = in ? ks[b + kNW * lane] : 0.0f;
+    vscales = in ? vs[b + kNW * lane] : 0.0f;
+  };
+  if (quant) {
+    load_scales(b0 + w);
+    load(kf, krs, b0 + w);
+    load(vf, vrs, b0 + w);
+  }
 
   // ---- the rows' queries into LDS: binary16, scaled, or bfloat16 as they are
   constexpr int TPR = D / 8;  // threads per row
@@ -163,22 +196,8 @@ __global__ __launch_bounds__(kT, 2) void k_attn_quant(QuantAttnArgs a) {
   float unscale = 1.0f;  // of the wave's output sums
 
   if (quant) {
-    const int b0 = (int)((int64_t)a.n_blocks * split / a.c8);
-    const int b1 = (int)((int64_t)a.n_blocks * (split + 1) / a.c8);
-    const float *ks = a.k_scale + (size_t)g * a.cap_blocks, *vs = a.v_scale + (size_t)g * a.cap_blocks;
-    const int bytes = a.cap_blocks * SB_KV_BLOCK * D;  // one head's codes: at most 2^27
-    const __amdgpu_buffer_rsrc_t krs = uniform_rsrc(a.k8 + (size_t)g * bytes, bytes);
-    const __amdgpu_buffer_rsrc_t vrs = uniform_rsrc(a.v8 + (size_t)g * bytes, bytes);
-    i32x4 kf[NF], vf[NF];
-    auto load = [&](i32x4 (&f)[NF], __amdgpu_buffer_rsrc_t rs, int b) {
-      const int vo = b < b1 ? b * (SB_KV_BLOCK * D) + lane * 16 : bytes;
-#pragma unroll
-      for (int i = 0; i < NF; ++i) f[i] = __builtin_amdgcn_raw_buffer_load_b128(rs, vo, i * 1024, 0);
-    };
-    load(kf, krs, b0 + w);
-    load(vf, vrs, b0 + w);
-    float vtop = 0.0f;
-    for (int b = b0 + w + kNW * lane; b < b1; b += kNW * 64) vtop = fmaxf(vtop, vs[b]);
+    float vtop = vscales;
+    for (int b = b0 + w + kNW * (64 + lane); b < b1; b += kNW * 64) vtop = fmaxf(vtop, vs[b]);
     for (int i = 32; i > 0; i >>= 1) vtop = fmaxf(vtop, __shfl_xor(vtop, i, 64));
     vtop = fmaxf(vtop, 0x1p-100f);  // every V block zero, or as good as
     unscale = vtop * 0x1p-15f;
@@ -186,8 +205,22 @@ __global__ __launch_bounds__(kT, 2) void k_attn_quant(QuantAttnArgs a) {
     float cq[RT];
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) cq[rt] = sqs[rt * 16 + lr];
+    int at = 0;  // lane that holds the block's scales
     for (int b = b0 + w; b < b1; b += kNW) {
-      const float kscale = ks[b], r = vs[b] * rv;
+      // the query fragments are read again for every block: in registers over the
+      // loop they would push others into memory
+      asm volatile("" ::: "memory");
+      if (at == 64) {
+        load_scales(b);
+        at = 0;
+      }
+      const float kscale = lane_value(kscales, at);
+      // r = vscale 2^15 / vtop, no smaller than 2^-25 (a block whose codes then
+      // count for less than 2^-40 of vtop each); a NaN stays
+      float r = lane_value(vscales, at) * rv;
+      r = r < 0x1p-25f ? 0x1p-25f : r;
+      const float lr2 = __builtin_amdgcn_logf(r), ir = 1.0f / r;
+      ++at;
       f32x4 s[RT][4];
 #pragma unroll
       for (int rt = 0; rt < RT; ++rt)
@@ -225,9 +258,8 @@ __global__ __launch_bounds__(kT, 2) void k_attn_quant(QuantAttnArgs a) {
           float x[8];
 #pragma unroll
           for (int e = 0; e < 8; ++e) {
-            x[e] = __builtin_amdgcn_exp2f(fmaf(s[rt][2 * h + (e >> 2)][e & 3], ck, -mc));
+            x[e] = __builtin_amdgcn_exp2f(fmaf(s[rt][2 * h + (e >> 2)][e & 3], ck, lr2 - mc));
             ps += x[e];
-            x[e] *= r;
           }
           uint4 pk;
           pk.x = pack_f16x2(x[0], x[1]);
@@ -236,7 +268,7 @@ __global__ __launch_bounds__(kT, 2) void k_attn_quant(QuantAttnArgs a) {
           pk.w = pack_f16x2(x[6], x[7]);
           p[rt][h] = __builtin_bit_cast(f16x8, pk);
         }
-        l[rt] += ps;
+        l[rt] = fmaf(ps, ir, l[rt]);
       }
 #pragma unroll
       for (int dt = 0; dt < NF; ++dt)
@@ -249,7 +281,7 @@ __global__ __launch_bounds__(kT, 2) void k_attn_quant(QuantAttnArgs a) {
       load(vf, vrs, b + kNW);
     }
   } else {
-    const int nkeys = a.tail_len + a.n_tok, n_steps = (nkeys + 31) >> 5, ts = split - a.c8;
+    const int nkeys = a.tail_len + a.n_tok, n_steps = (nkeys + 31) >> 5, ts = split;
     const int st0 = n_steps * ts / a.ct, st1 = n_steps * (ts + 1) / a.ct;
     const int bytes = a.tail_cap * D * 2;
     const __amdgpu_buffer_rsrc_t krs = uniform_rsrc(a.tk + (size_t)g * a.tail_cap * D, bytes);
@@ -402,7 +434,7 @@ __global__ __launch_bounds__(SB_MAX_ROWS) void k_tree_masks(Meta *meta, TreeArg 
 
 template <int D, int FMT>
 hipError_t launch_rt(const QuantAttnArgs &a, int rt, hipStream_t s) {
-  const dim3 grid(a.n_kv * a.n_chunks * a.n_rb), block(kT);
+  const dim3 grid(round_up(a.n_kv * a.n_chunks, 8) * a.n_rb), block(kT);
   switch (rt) {
     case 1: hipLaunchKernelGGL((k_attn_quant<D, FMT, 1>), grid, block, 0, s, a); break;
     case 2: hipLaunchKernelGGL((k_attn_quant<D, FMT, 2>), grid, block, 0, s, a); break;
@@ -429,12 +461,9 @@ QuantAttnPlan quant_attn_plan(int n_kv, int n_blocks, int tail_keys, int rows) {
   p.ct = (int)((int64_t)per * steps / (n_blocks + steps));
   if (p.ct > ceil_div(steps, kNW)) p.ct = ceil_div(steps, kNW);
   if (p.ct < 1) p.ct = 1;
-  p.c8 = per - p.ct;
+  p.c8 = per - (p.ct > 1 ? p.ct : 0);
   if (p.c8 > ceil_div(n_blocks, kNW)) p.c8 = ceil_div(n_blocks, kNW);
-  if (p.c8 < 1 && n_blocks > 0) {
-    p.c8 = 1;
-    p.ct = per - 1;
-  }
+  if (p.c8 < 1 && n_blocks > 0) p.c8 = 1;
   return p;
 }
 
