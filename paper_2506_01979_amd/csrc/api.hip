@@ -417,7 +417,7 @@ sb_status forward_bf16(sb_model *m, const sb_kv_cache *kv, int kv_len, const int
     if (quant) {
       const QuantAttnArgs qa =
           quant_attn_args(c, *quant->kv, l, quant->n_blocks, kv_len, n, q, meta, ws, L);
-      SB_TIMED(SB_KC_ATTN, launch_attn_quant(qa, s));
+      SB_TIMED(SB_KC_ATTN, launch_attn_quant(qa, tree, s));
       SB_TIMED(SB_KC_ATTN_MERGE, launch_attn_merge_bf16(quant_merge_args(qa), xa, L.ks_o, s));
     } else {
       SB_TIMED(SB_KC_ATTN, launch_attn_bf16(aa, s));
@@ -567,7 +567,7 @@ sb_status forward_int8(sb_model *m, const sb_kv_cache *kv, int kv_len, const int
     if (quant) {
       const QuantAttnArgs qa =
           quant_attn_args(c, *quant->kv, l, quant->n_blocks, kv_len, n, q, meta, ws, L);
-      SB_TIMED(SB_KC_ATTN, launch_attn_quant(qa, s));
+      SB_TIMED(SB_KC_ATTN, launch_attn_quant(qa, tree, s));
       SB_TIMED(SB_KC_ATTN_MERGE, launch_attn_merge_bf16(quant_merge_args(qa), ao, 0, s));
     } else {
       aa.kc = ra.kc;
@@ -1653,10 +1653,9 @@ sb_status sb_kv_commit(const sb_model_config *cfg, const sb_quantized_kv *kv, in
   return SB_OK;
 }
 
-// Workspace of the attention by itself: the tree's masks, the partials.
+// Workspace of the attention by itself: the partials.
 static Layout attend_layout(const sb_model_config &c, int n_rows, int n_blocks, int tail_len) {
   Layout L{};
-  L.total = align_up(sizeof(Meta));
   take_quant_partials(c, n_rows, n_blocks, tail_len, &L);
   return L;
 }
@@ -1697,11 +1696,9 @@ sb_status sb_attend_quantized(const sb_model_config *cfg, const sb_quantized_kv 
   if ((st = check_quant_step(kv, n_blocks, tail_len, n_rows)) != SB_OK) return st;
   const Layout L = attend_layout(*cfg, n_rows, n_blocks, tail_len);
   if (ws_bytes < L.total) return SB_ERR_CAPACITY;
-  Meta *meta = (Meta *)d_ws;
-  const QuantAttnArgs a = quant_attn_args(*cfg, *kv, layer, n_blocks, tail_len, n_rows, d_q, meta,
-                                          (char *)d_ws, L);
-  SB_TRY(launch_tree_masks(meta, tree, stream));
-  SB_TRY(launch_attn_quant(a, stream));
+  const QuantAttnArgs a = quant_attn_args(*cfg, *kv, layer, n_blocks, tail_len, n_rows, d_q,
+                                          nullptr, (char *)d_ws, L);
+  SB_TRY(launch_attn_quant(a, tree, stream));
   return hip_status(launch_attn_merge_bf16(quant_merge_args(a), (uint16_t *)d_out, 0, stream));
 }
 

@@ -75,13 +75,62 @@ __device__ __forceinline__ f16x8 widen8(uint32_t w0, uint32_t w1) {
   return __builtin_bit_cast(f16x8, o);
 }
 
+// The largest of three (a NaN is passed over), one instruction; from fmaxf the
+// compiler first makes quiet copies of its arguments.
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+  return r;
+}
+
 __device__ __forceinline__ float lane_value(float v, int lane) {
   return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), lane));
 }
 
+// The ancestor masks of the workgroup's rows into sanc: from the step's
+// metadata where the caller has it, else from the tree, every row's at once in
+// log2(n) rounds (a row takes over its jump's ancestors, then all jumps double).
+// all: SB_MAX_ROWS masks of scratch; one thread per row.
+static_assert(kT == SB_MAX_ROWS, "a thread per tree row");
+template <int RT>
+__device__ __forceinline__ void stage_masks(const QuantAttnArgs &a, const TreeArg &tree, int rb,
+                                            int R, float inv_g, uint32_t (*sanc)[8],
+                                            uint32_t (*all)[8]) {
+  constexpr int RB = 16 * RT;
+  __shared__ int16_t s_jump[SB_MAX_ROWS];
+  if (!a.meta) {
+    const int i = threadIdx.x;
+    int jump = i < tree.n ? tree.parent[i] : -1;
+    uint32_t on[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      on[k] = (i >> 5) == k ? 1u << (i & 31) : 0u;
+      all[i][k] = on[k];
+    }
+    s_jump[i] = (int16_t)jump;
+    __syncthreads();
+    for (int step = 1; step < tree.n; step <<= 1) {
+      const int next = jump >= 0 ? s_jump[jump] : -1;
+      if (jump >= 0)
+#pragma unroll
+        for (int k = 0; k < 8; ++k) on[k] |= all[jump][k];
+      __syncthreads();
+      jump = next;
+      s_jump[i] = (int16_t)next;
+#pragma unroll
+      for (int k = 0; k < 8; ++k) all[i][k] = on[k];
+      __syncthreads();
+    }
+  }
+  for (int i = threadIdx.x; i < RB * 8; i += kT) {
+    const int r = rb * RB + (i >> 3), t = (int)(((float)r + 0.5f) * inv_g);
+    sanc[i >> 3][i & 7] = r < R ? (a.meta ? a.meta->anc[t][i & 7] : all[t][i & 7]) : 0u;
+  }
+}
+
 // D: head_dim; RT: 16-row query tiles of the workgroup.
 template <int D, int FMT, int RT>
-__global__ __launch_bounds__(kT, 2) void k_attn_quant(QuantAttnArgs a) {
+__global__ __launch_bounds__(kT, 2) void k_attn_quant(QuantAttnArgs a, TreeArg tree) {
   constexpr int KSD = D / 32;  // k-steps over head_dim (S)
   constexpr int NF = D / 16;   // fragments of K, or V, of a block; output tiles
   constexpr int RB = 16 * RT;
@@ -136,39 +185,47 @@ __global__ __launch_bounds__(kT, 2) void k_attn_quant(QuantAttnArgs a) {
 
   // ---- the rows' queries into LDS: binary16, scaled, or bfloat16 as they are
   constexpr int TPR = D / 8;  // threads per row
-  for (int i = threadIdx.x; i < RB * TPR; i += kT) {
-    const int rr = i / TPR, d0 = (i % TPR) * 8;
-    const int r = rb * RB + rr, t = r / G;
-    uint4 x = make_uint4(0, 0, 0, 0);
-    if (r < R)
-      x = *(const uint4 *)((const uint16_t *)a.q + ((size_t)t * a.n_heads + g * G + (r - t * G)) * D + d0);
+  constexpr int QPT = (RB * TPR + kT - 1) / kT;
+  const float inv_g = 1.0f / (float)G;  // r / G = floor((r + 0.5) / G) for r < 2^20
+  uint4 xq[QPT];
+#pragma unroll
+  for (int j = 0; j < QPT; ++j) {
+    const int i = threadIdx.x + j * kT, r = rb * RB + i / TPR;
+    const int t = (int)(((float)r + 0.5f) * inv_g);
+    xq[j] = make_uint4(0, 0, 0, 0);
+    if (i < RB * TPR && r < R)
+      xq[j] = *(const uint4 *)((const uint16_t *)a.q +
+                               ((size_t)t * a.n_heads + g * G + (r - t * G)) * D + (i % TPR) * 8);
+  }
+#pragma unroll
+  for (int j = 0; j < QPT; ++j) {
+    const int i = threadIdx.x + j * kT, rr = i / TPR, d0 = (i % TPR) * 8;
+    if (i >= RB * TPR) break;  // whole waves
+    uint4 x = xq[j];
     if (quant) {
       const uint32_t xw[4] = {x.x, x.y, x.z, x.w};
       uint32_t top = 0;
 #pragma unroll
       for (int e = 0; e < 4; ++e) top = max(top, max(xw[e] & 0x7fffu, (xw[e] >> 16) & 0x7fffu));
+#pragma unroll
       for (int o = TPR / 2; o > 0; o >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, o, 64));
       // 2^(14 - e) for a largest magnitude in [2^e, 2^(e + 1)), e >= -100
       int e = (int)(top >> 7) - 127;
       e = e < -100 ? -100 : e;
-      const float f = ldexpf(1.0f, 14 - e);
+      const float f = __uint_as_float((uint32_t)(127 + 14 - e) << 23);
       uint4 o;
       o.x = pack_f16x2(bf2f((uint16_t)xw[0]) * f, bf2f((uint16_t)(xw[0] >> 16)) * f);
       o.y = pack_f16x2(bf2f((uint16_t)xw[1]) * f, bf2f((uint16_t)(xw[1] >> 16)) * f);
       o.z = pack_f16x2(bf2f((uint16_t)xw[2]) * f, bf2f((uint16_t)(xw[2] >> 16)) * f);
       o.w = pack_f16x2(bf2f((uint16_t)xw[3]) * f, bf2f((uint16_t)(xw[3] >> 16)) * f);
       x = o;
-      if (d0 == 0) sqs[rr] = c * ldexpf(1.0f, e - 14);
+      if (d0 == 0) sqs[rr] = c * __uint_as_float((uint32_t)(127 + e - 14) << 23);
     } else if (d0 == 0) {
       sqs[rr] = c;
     }
     *(uint4 *)&sq[rr][d0] = x;
   }
-  if (!quant)
-    for (int i = threadIdx.x; i < RB * 8; i += kT) {
-      const int r = rb * RB + (i >> 3);
-      sanc[i >> 3][i & 7] = r < R ? a.meta->anc[r / G][i & 7] : 0u;
-    }
+  if (!quant) stage_masks<RT>(a, tree, rb, R, inv_g, sanc, (uint32_t (*)[8]) & so[0][0][0]);
   __syncthreads();
 
   f32x4 o[RT][NF];
@@ -180,18 +237,23 @@ __global__ __launch_bounds__(kT, 2) void k_attn_quant(QuantAttnArgs a) {
     m[rt] = -INFINITY;
     l[rt] = 0.0f;
   }
-  // A larger maximum nm of row tile rt: the sums so far scale down (from -inf:
-  // to 0).
-  auto raise = [&](int rt, float nm) {
-    nm = fmaxf(m[rt], nm);
-    if (__ballot(nm > m[rt])) {
-      const float f = m[rt] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m[rt] - nm);
-      m[rt] = nm;
-      l[rt] *= f;
+  // Row maxima nm: where one is larger than before, every sum so far scales down
+  // to it (from -inf: to 0).  One branch for the row tiles together.
+  auto raise = [&](float (&nm)[RT]) {
+    bool more = false;
 #pragma unroll
-      for (int dt = 0; dt < NF; ++dt) o[rt][dt] *= f;
+    for (int rt = 0; rt < RT; ++rt) more |= nm[rt] > m[rt];
+    if (__ballot(more)) {
+#pragma unroll
+      for (int rt = 0; rt < RT; ++rt) {
+        const float top = fmaxf(m[rt], nm[rt]);
+        const float f = m[rt] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m[rt] - top);
+        m[rt] = top;
+        l[rt] *= f;
+#pragma unroll
+        for (int dt = 0; dt < NF; ++dt) o[rt][dt] *= f;
+      }
     }
-    return m[rt] == -INFINITY ? 0.0f : m[rt];
   };
   float unscale = 1.0f;  // of the wave's output sums
 
@@ -202,9 +264,6 @@ __global__ __launch_bounds__(kT, 2) void k_attn_quant(QuantAttnArgs a) {
     vtop = fmaxf(vtop, 0x1p-100f);  // every V block zero, or as good as
     unscale = vtop * 0x1p-15f;
     const float rv = 0x1p15f / vtop;
-    float cq[RT];
-#pragma unroll
-    for (int rt = 0; rt < RT; ++rt) cq[rt] = sqs[rt * 16 + lr];
     int at = 0;  // lane that holds the block's scales
     for (int b = b0 + w; b < b1; b += kNW) {
       // the query fragments are read again for every block: in registers over the
@@ -239,26 +298,33 @@ __global__ __launch_bounds__(kT, 2) void k_attn_quant(QuantAttnArgs a) {
 #pragma unroll
           for (int rt = 0; rt < RT; ++rt) s[rt][kt] = mfma16h(kv, qv[rt], s[rt][kt]);
         }
+        // one k-step's query fragments at a time: with more of them early, RT = 3
+        // has registers in memory, whose loads wait for the cache's
+        if (RT == 3) __builtin_amdgcn_sched_barrier(0);
       }
       load(kf, krs, b + kNW);
       // ---- softmax: element e of s[rt][2 h + i] is key 32 h + 8 lg + 4 i + e
       f16x8 p[RT][2];
+      float ck[RT], nm[RT];
 #pragma unroll
       for (int rt = 0; rt < RT; ++rt) {
-        float mx = -INFINITY;
+        float mx = fmaxf(s[rt][0][0], s[rt][0][1]);
 #pragma unroll
-        for (int kt = 0; kt < 4; ++kt)
-          mx = fmaxf(mx, fmaxf(fmaxf(s[rt][kt][0], s[rt][kt][1]), fmaxf(s[rt][kt][2], s[rt][kt][3])));
-        mx = max_x32(max_x16(mx));
-        const float ck = cq[rt] * kscale;
-        const float mc = raise(rt, mx * ck);
+        for (int e = 2; e < 16; e += 2) mx = max3(mx, s[rt][e >> 2][e & 3], s[rt][e >> 2][(e & 3) + 1]);
+        ck[rt] = sqs[rt * 16 + lr] * kscale;
+        nm[rt] = max_x32(max_x16(mx)) * ck[rt];
+      }
+      raise(nm);
+#pragma unroll
+      for (int rt = 0; rt < RT; ++rt) {
+        const float base = lr2 - (m[rt] == -INFINITY ? 0.0f : m[rt]);
         float ps = 0.0f;
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
           float x[8];
 #pragma unroll
           for (int e = 0; e < 8; ++e) {
-            x[e] = __builtin_amdgcn_exp2f(fmaf(s[rt][2 * h + (e >> 2)][e & 3], ck, lr2 - mc));
+            x[e] = __builtin_amdgcn_exp2f(fmaf(s[rt][2 * h + (e >> 2)][e & 3], ck[rt], base));
             ps += x[e];
           }
           uint4 pk;
@@ -269,6 +335,7 @@ __global__ __launch_bounds__(kT, 2) void k_attn_quant(QuantAttnArgs a) {
           p[rt][h] = __builtin_bit_cast(f16x8, pk);
         }
         l[rt] = fmaf(ps, ir, l[rt]);
+        if (RT == 3) __builtin_amdgcn_sched_barrier(0);
       }
 #pragma unroll
       for (int dt = 0; dt < NF; ++dt)
@@ -322,22 +389,29 @@ __global__ __launch_bounds__(kT, 2) void k_attn_quant(QuantAttnArgs a) {
           for (int e = 0; e < 4; ++e)
             vf[dt][e] &= (int)((2 * e < valid ? 0x0000ffffu : 0u) | (2 * e + 1 < valid ? 0xffff0000u : 0u));
       }
+      float nm[RT];
 #pragma unroll
       for (int rt = 0; rt < RT; ++rt) {
         const uint32_t vis = visible8(sanc[rt * 16 + lr], k0, a.tail_len, nkeys);
-        float x[8], mx = -INFINITY;
+        float mx = -INFINITY;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          x[e] = (vis >> e) & 1u ? s[rt][e >> 2][e & 3] : -INFINITY;
-          mx = fmaxf(mx, x[e]);
+          const float x = (vis >> e) & 1u ? s[rt][e >> 2][e & 3] : -INFINITY;
+          s[rt][e >> 2][e & 3] = x;
+          mx = fmaxf(mx, x);
         }
-        mx = max_x32(max_x16(mx));
-        const float mc = raise(rt, mx * c);
+        nm[rt] = max_x32(max_x16(mx)) * c;
+      }
+      raise(nm);
+#pragma unroll
+      for (int rt = 0; rt < RT; ++rt) {
+        const float mc = m[rt] == -INFINITY ? 0.0f : m[rt];
+        float x[8];
         float ps = 0.0f;
         uint32_t hi[4], lo[4];
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          x[e] = __builtin_amdgcn_exp2f(fmaf(x[e], c, -mc));  // exp2(-inf) = 0 when masked
+          x[e] = __builtin_amdgcn_exp2f(fmaf(s[rt][e >> 2][e & 3], c, -mc));  // exp2(-inf) = 0 when masked
           ps += x[e];
         }
 #pragma unroll
@@ -410,35 +484,13 @@ __global__ __launch_bounds__(kT, 2) void k_attn_quant(QuantAttnArgs a) {
   }
 }
 
-// The ancestor masks of a tree (Meta::anc), one workgroup per row: round r
-// marks the 2^r-th ancestors of the rows marked so far, then all jumps double.
-__global__ __launch_bounds__(SB_MAX_ROWS) void k_tree_masks(Meta *meta, TreeArg tree) {
-  __shared__ int16_t s_jump[SB_MAX_ROWS];
-  __shared__ uint8_t s_on[SB_MAX_ROWS];
-  int jump = (int)threadIdx.x < tree.n ? tree.parent[threadIdx.x] : -1;
-  s_jump[threadIdx.x] = (int16_t)jump;
-  s_on[threadIdx.x] = threadIdx.x == blockIdx.x;
-  __syncthreads();
-  for (int step = 1; step < tree.n; step <<= 1) {
-    const int next = jump >= 0 ? s_jump[jump] : -1;
-    if (jump >= 0 && s_on[threadIdx.x]) s_on[jump] = 1;
-    __syncthreads();
-    jump = next;
-    s_jump[threadIdx.x] = (int16_t)next;
-    __syncthreads();
-  }
-  const unsigned long long on = __ballot(s_on[threadIdx.x] != 0);
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-  if (lane < 2) meta->anc[blockIdx.x][2 * w + lane] = (uint32_t)(on >> (32 * lane));
-}
-
 template <int D, int FMT>
-hipError_t launch_rt(const QuantAttnArgs &a, int rt, hipStream_t s) {
+hipError_t launch_rt(const QuantAttnArgs &a, const TreeArg &tree, int rt, hipStream_t s) {
   const dim3 grid(round_up(a.n_kv * a.n_chunks, 8) * a.n_rb), block(kT);
   switch (rt) {
-    case 1: hipLaunchKernelGGL((k_attn_quant<D, FMT, 1>), grid, block, 0, s, a); break;
-    case 2: hipLaunchKernelGGL((k_attn_quant<D, FMT, 2>), grid, block, 0, s, a); break;
-    case 3: hipLaunchKernelGGL((k_attn_quant<D, FMT, 3>), grid, block, 0, s, a); break;
+    case 1: hipLaunchKernelGGL((k_attn_quant<D, FMT, 1>), grid, block, 0, s, a, tree); break;
+    case 2: hipLaunchKernelGGL((k_attn_quant<D, FMT, 2>), grid, block, 0, s, a, tree); break;
+    case 3: hipLaunchKernelGGL((k_attn_quant<D, FMT, 3>), grid, block, 0, s, a, tree); break;
     default: return hipErrorInvalidValue;
   }
   return hipGetLastError();
@@ -467,12 +519,7 @@ QuantAttnPlan quant_attn_plan(int n_kv, int n_blocks, int tail_keys, int rows) {
   return p;
 }
 
-hipError_t launch_tree_masks(Meta *meta, const TreeArg &tree, hipStream_t s) {
-  hipLaunchKernelGGL(k_tree_masks, dim3(tree.n), dim3(SB_MAX_ROWS), 0, s, meta, tree);
-  return hipGetLastError();
-}
-
-hipError_t launch_attn_quant(const QuantAttnArgs &args, hipStream_t s) {
+hipError_t launch_attn_quant(const QuantAttnArgs &args, const TreeArg &tree, hipStream_t s) {
   QuantAttnArgs a = args;
   const QuantAttnPlan p =
       quant_attn_plan(a.n_kv, a.n_blocks, a.tail_len + a.n_tok, a.n_tok * (a.n_heads / a.n_kv));
@@ -481,11 +528,11 @@ hipError_t launch_attn_quant(const QuantAttnArgs &args, hipStream_t s) {
   a.ct = p.ct;
   a.n_rb = p.n_rb;
   if (a.head_dim == 128)
-    return a.format == SB_KV_INT8 ? launch_rt<128, SB_KV_INT8>(a, p.rt, s)
-                                  : launch_rt<128, SB_KV_E4M3>(a, p.rt, s);
+    return a.format == SB_KV_INT8 ? launch_rt<128, SB_KV_INT8>(a, tree, p.rt, s)
+                                  : launch_rt<128, SB_KV_E4M3>(a, tree, p.rt, s);
   if (a.head_dim == 64)
-    return a.format == SB_KV_INT8 ? launch_rt<64, SB_KV_INT8>(a, p.rt, s)
-                                  : launch_rt<64, SB_KV_E4M3>(a, p.rt, s);
+    return a.format == SB_KV_INT8 ? launch_rt<64, SB_KV_INT8>(a, tree, p.rt, s)
+                                  : launch_rt<64, SB_KV_E4M3>(a, tree, p.rt, s);
   return hipErrorInvalidValue;
 }
 

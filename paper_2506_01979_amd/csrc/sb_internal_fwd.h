@@ -297,7 +297,7 @@ hipError_t launch_kv_move(uint16_t *k, uint16_t *v, int heads, int cap, int head
 // merge kernels take 512).
 constexpr int kQuantTargetGroups = 512;
 constexpr int kQuantMaxRowTiles = 3;
-constexpr int kQuantMaxRanges = 256;
+constexpr int kQuantMaxRanges = 31;
 struct QuantAttnPlan {
   int rt, n_rb, c8, ct;  // row tiles and row blocks; ranges of the blocks and of the tail
 };
@@ -312,12 +312,11 @@ struct QuantAttnArgs {
   int n_tok, n_heads, n_kv, head_dim;
   int n_chunks;             // c8 + ct of the plan
   int c8, ct, n_rb;         // filled in by the launch
-  const Meta *meta;         // ancestor masks
+  const Meta *meta;         // ancestor masks; null: the kernel finds them itself
   float scale;
   float *part_o, *part_ml;  // as AttnArgs
 };
-hipError_t launch_tree_masks(Meta *meta, const TreeArg &tree, hipStream_t s);
-hipError_t launch_attn_quant(const QuantAttnArgs &a, hipStream_t s);
+hipError_t launch_attn_quant(const QuantAttnArgs &a, const TreeArg &tree, hipStream_t s);
 
 // ---- 8-bit projections (k_linear.hip) ------------------------------------------
 // Most inputs of a projection (a row of it is held in registers), most token
