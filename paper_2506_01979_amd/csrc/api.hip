@@ -251,19 +251,19 @@ struct TimedLaunch {
     SB_TRY(expr);                   \
   } while (0)
 
-// Partials of the attention over a quantised cache: room for every call of at
-// most n_rows rows, n_blocks blocks and tail_len tail slots (ranges x rows of a
-// KV head: quant_attn_plan's ranges are at most kQuantTargetGroups over the KV
-// heads and row blocks, or 2, and one more, and a range has four steps).
+// Partials (key ranges x rows x KV heads) of the attention over a quantised
+// cache, behind what the layout holds already; up_to: with room for every call of
+// at most n_rows rows, n_blocks blocks and tail_len tail slots (the ranges grow
+// with the steps; with the rows they may fall).
 void take_quant_partials(const sb_model_config &c, int n_rows, int n_blocks, int tail_len,
-                         Layout *L) {
-  const int64_t rows = (int64_t)n_rows * (c.n_heads / c.n_kv_heads);
-  const int64_t per_block = 16 * kQuantMaxRowTiles;
-  int64_t parts = kQuantTargetGroups * (rows < per_block ? rows : per_block);
-  if (parts < 2 * c.n_kv_heads * rows) parts = 2 * c.n_kv_heads * rows;
-  parts += c.n_kv_heads * rows;
-  const int64_t ranges = ceil_div(n_blocks, 4) + ceil_div(ceil_div(tail_len + n_rows, 32), 4);
-  if (parts > ranges * c.n_kv_heads * rows) parts = ranges * c.n_kv_heads * rows;
+                         bool up_to, Layout *L) {
+  const int G = c.n_heads / c.n_kv_heads;
+  int64_t parts = 0;
+  for (int n = up_to ? 1 : n_rows; n <= n_rows; ++n) {
+    const int64_t p = (int64_t)quant_attn_plan(c.n_kv_heads, c.head_dim, n_blocks, tail_len + n, n * G).chunks *
+                      c.n_kv_heads * n * G;
+    if (p > parts) parts = p;
+  }
   L->quant_o = L->total;
   L->quant_ml = align_up(L->quant_o + parts * c.head_dim * sizeof(float));
   L->total = align_up(L->quant_ml + parts * 2 * sizeof(float));
@@ -283,7 +283,7 @@ QuantAttnArgs quant_attn_args(const sb_model_config &c, const sb_quantized_kv &k
   const size_t codes = heads * kv.capacity * c.head_dim;
   const size_t tail = heads * kv.tail.capacity * c.head_dim;
   const QuantAttnPlan p =
-      quant_attn_plan(c.n_kv_heads, n_blocks, tail_len + n_rows, n_rows * (c.n_heads / c.n_kv_heads));
+      quant_attn_plan(c.n_kv_heads, c.head_dim, n_blocks, tail_len + n_rows, n_rows * (c.n_heads / c.n_kv_heads));
   QuantAttnArgs a{};
   a.q = q;
   a.cap_blocks = (int)cap_blocks;
@@ -303,7 +303,7 @@ QuantAttnArgs quant_attn_args(const sb_model_config &c, const sb_quantized_kv &k
   a.n_heads = c.n_heads;
   a.n_kv = c.n_kv_heads;
   a.head_dim = c.head_dim;
-  a.n_chunks = p.c8 + p.ct;
+  a.n_chunks = p.chunks;
   a.meta = meta;
   a.scale = 1.0f / sqrtf((float)c.head_dim);
   a.part_o = (float *)(ws + L.quant_o);
@@ -1654,9 +1654,10 @@ sb_status sb_kv_commit(const sb_model_config *cfg, const sb_quantized_kv *kv, in
 }
 
 // Workspace of the attention by itself: the partials.
-static Layout attend_layout(const sb_model_config &c, int n_rows, int n_blocks, int tail_len) {
+static Layout attend_layout(const sb_model_config &c, int n_rows, int n_blocks, int tail_len,
+                            bool up_to) {
   Layout L{};
-  take_quant_partials(c, n_rows, n_blocks, tail_len, &L);
+  take_quant_partials(c, n_rows, n_blocks, tail_len, up_to, &L);
   return L;
 }
 
@@ -1669,7 +1670,7 @@ size_t sb_attend_workspace_bytes(const sb_model_config *cfg, int32_t max_rows, i
                                  int32_t max_tail_len) {
   if (check_attention_config(cfg) != SB_OK || !quant_sizes_ok(max_rows, max_blocks, max_tail_len))
     return 0;
-  return attend_layout(*cfg, max_rows, max_blocks, max_tail_len).total;
+  return attend_layout(*cfg, max_rows, max_blocks, max_tail_len, true).total;
 }
 
 // What both attention calls check of the cache.
@@ -1694,7 +1695,7 @@ sb_status sb_attend_quantized(const sb_model_config *cfg, const sb_quantized_kv 
   TreeArg tree;
   if ((st = check_tree(h_parents, n_rows, &tree)) != SB_OK) return st;
   if ((st = check_quant_step(kv, n_blocks, tail_len, n_rows)) != SB_OK) return st;
-  const Layout L = attend_layout(*cfg, n_rows, n_blocks, tail_len);
+  const Layout L = attend_layout(*cfg, n_rows, n_blocks, tail_len, false);
   if (ws_bytes < L.total) return SB_ERR_CAPACITY;
   const QuantAttnArgs a = quant_attn_args(*cfg, *kv, layer, n_blocks, tail_len, n_rows, d_q,
                                           nullptr, (char *)d_ws, L);
@@ -1707,7 +1708,7 @@ sb_status sb_attend_quantized(const sb_model_config *cfg, const sb_quantized_kv 
 static Layout quant_forward_layout(const sb_model_config &c, int n_rows, int n_blocks, int tail_len,
                                    bool up_to) {
   Layout L = make_layout(c, n_rows, tail_len, up_to);
-  take_quant_partials(c, n_rows, n_blocks, tail_len, &L);
+  take_quant_partials(c, n_rows, n_blocks, tail_len, up_to, &L);
   return L;
 }
 

@@ -292,16 +292,14 @@ hipError_t launch_kv_dequantize(const QuantKvArgs &a, hipStream_t s);
 hipError_t launch_kv_move(uint16_t *k, uint16_t *v, int heads, int cap, int head_dim, int from,
                           int n, hipStream_t s);
 
-// Attention of one layer over a quantised cache.  Workgroups planned for
-// (two per compute unit), most 16-row query tiles of one, most key ranges (the
-// merge kernels take 512).
-constexpr int kQuantTargetGroups = 512;
-constexpr int kQuantMaxRowTiles = 3;
-constexpr int kQuantMaxRanges = 31;
+// Attention of one layer over a quantised cache: most key ranges (the merge in
+// registers takes 32).
+constexpr int kQuantMaxRanges = 32;
+// rt row tiles per wave, row blocks, key ranges per KV head.
 struct QuantAttnPlan {
-  int rt, n_rb, c8, ct;  // row tiles and row blocks; ranges of the blocks and of the tail
+  int rt, n_rb, chunks;
 };
-QuantAttnPlan quant_attn_plan(int n_kv, int n_blocks, int tail_keys, int rows);
+QuantAttnPlan quant_attn_plan(int n_kv, int head_dim, int n_blocks, int tail_keys, int rows);
 struct QuantAttnArgs {
   const void *q;            // bf16 [rows][n_heads][d]
   const uint8_t *k8, *v8;   // this layer's codes
@@ -310,8 +308,8 @@ struct QuantAttnArgs {
   const uint16_t *tk, *tv;  // this layer's tail
   int tail_cap, tail_len;
   int n_tok, n_heads, n_kv, head_dim;
-  int n_chunks;             // c8 + ct of the plan
-  int c8, ct, n_rb;         // filled in by the launch
+  int n_chunks;             // key ranges of the plan
+  int n_rb;                 // filled in by the launch
   const Meta *meta;         // ancestor masks; null: the kernel finds them itself
   float scale;
   float *part_o, *part_ml;  // as AttnArgs
