@@ -56,8 +56,8 @@ struct Layout {
   size_t xa, act, q, part_o, part_ml, xn, ss, rs, pk_table, pk_sync;
   // f32
   size_t fq, fo, fact;
-  // int8: a projection's output, the codes and scales of its input
-  size_t y, xq, xs, ao;
+  // int8: a projection's output, the codes and scales of its input, its K ranges' sums
+  size_t y, xq, xs, ao, lin_part;
   // attention over a quantised cache: partials of both its parts
   size_t quant_o, quant_ml;
   size_t total;
@@ -125,6 +125,13 @@ Layout make_layout(const sb_model_config &c, int n_rows, int kv_len, bool up_to 
       L.xq = take((size_t)np * most * 64);
       L.xs = take((size_t)np * sizeof(float));
       L.ao = take((size_t)np * qd * 2);
+      size_t part = 0;
+      for (const int kind : {SB_W_QKV, SB_W_O, SB_W_GATE_UP, SB_W_DOWN, SB_W_LM_HEAD}) {
+        const PackGeom g = pack_geom(c, kind);
+        const size_t b = linear_part_bytes(g.rows, g.K, n_rows);
+        if (b > part) part = b;
+      }
+      L.lin_part = take(part);
       L.total = off;
       return L;
     }
@@ -530,6 +537,7 @@ sb_status forward_int8(sb_model *m, const sb_kv_cache *kv, int kv_len, const int
     a.tiles = g.tiles;
     a.ks = g.ks;
     a.n_tok = n;
+    a.part = (int32_t *)(ws + L.lin_part);
     return launch_linear(a, s);
   };
   RopeStoreArgs ra{};
@@ -1835,7 +1843,8 @@ sb_status sb_linear_pack(int32_t m, int32_t k, const void *d_w, void *d_packed,
 size_t sb_linear_workspace_bytes(int32_t m, int32_t k, int32_t max_rows) {
   if (!linear_ok(m, k) || max_rows < 1 || max_rows > SB_MAX_ROWS) return 0;
   const size_t rows = round_up(max_rows, 16);
-  return align_up(rows * linear_geom(m, k).ks * 64) + align_up(rows * sizeof(float));
+  return align_up(rows * linear_geom(m, k).ks * 64) + align_up(rows * sizeof(float)) +
+         linear_part_bytes(m, k, max_rows);
 }
 
 sb_status sb_linear_quantized(int32_t m, int32_t k, const void *d_packed, int32_t n_rows,
@@ -1859,6 +1868,7 @@ sb_status sb_linear_quantized(int32_t m, int32_t k, const void *d_packed, int32_
   a.tiles = g.tiles;
   a.ks = g.ks;
   a.n_tok = n_rows;
+  a.part = (int32_t *)((char *)scales + align_up((size_t)round_up(n_rows, 16) * sizeof(float)));
   SB_TRY(launch_quant_rows(d_x, x_dtype == SB_BF16, n_rows, k, codes, scales, stream));
   return hip_status(launch_linear(a, stream));
 }

@@ -2,13 +2,19 @@
 // codes in [-127, 127] with a scale per token and per output channel, sums in
 // 32-bit integers (exact for up to 2^17 inputs).
 //
-// The product streams every weight tile (16 channels) from HBM once, 16 bytes
-// per lane and k-step of 64 in the operand order of the 16x16x64 integer
-// matrix instruction, straight into registers; the activations (all rows: at
-// most 256 x 28672 bytes) come the same way out of the L2.  A workgroup owns NT
-// weight tiles and TT token tiles; its waves split K, so every wave streams its
-// own stretch of the tiles with nothing shared until the end, where the waves'
-// sums meet in LDS.
+// What bounds it: the weights' bytes, m k, read once, up to some 100 rows; then the
+// activations' way to the compute units, as every workgroup reads all n k of them
+// from the L2.  Weights and activations lie in the operand order of the 16x16x64
+// integer matrix instruction, 16 bytes per lane and k-step of 64, tiles of 16
+// channels or tokens.  Two kernels (linear_plan has the rule and both sides'
+// times):
+// - k_linear, few rows: both operands straight to registers; a workgroup owns NT
+//   weight tiles and TT token tiles, its waves split K, so every wave streams its
+//   own stretch of the tiles with nothing shared until the end, where the waves'
+//   sums meet in LDS.  22016 x 4096, 33 rows: 23.4 us, 3.9 TB/s.
+// - k_linear_ring, many rows: 128 or 256 channels and all rows per workgroup, so
+//   that activations are read once per that many channels; both operands through
+//   a ring of LDS stages.  57344 x 8192, 129 rows: 114 us, 4.3 TB/s (k_linear: 172).
 #include <math.h>
 
 #include "sb_internal_fwd.h"
@@ -143,6 +149,22 @@ __device__ __forceinline__ i32x4 mfma16i(i32x4 a, i32x4 b, i32x4 c) {
   return __builtin_amdgcn_mfma_i32_16x16x64_i8(a, b, c, 0, 0, 0);
 }
 
+// Outputs r .. r + 3 (r a multiple of 4) of token t from their sums.
+__device__ __forceinline__ void store_scaled(const LinearArgs &a, int t, int r, i32x4 v, f32x4 sw) {
+  const float sx = a.x_scale[t];
+  f32x4 y;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) y[e] = (float)v[e] * (sx * sw[e]);
+  float *dst = a.y + (size_t)t * a.m + r;
+  if (a.vec && r < a.m) {
+    *(f32x4 *)dst = y;
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (r + e < a.m) dst[e] = y[e];
+  }
+}
+
 // NT weight tiles x TT token tiles, NW waves; kU k-steps are in flight while
 // the kU before them are multiplied.
 constexpr int kU = 2;
@@ -220,21 +242,113 @@ __global__ __launch_bounds__(64 * NW) void k_linear(LinearArgs a) {
       for (int k = 1; k < NW; ++k) v += red[k][i >> 6][ln];
       const int r = (tile0 + p / TT) * 16 + 4 * (ln >> 4), t = (tt0 + p % TT) * 16 + (ln & 15);
       if (t >= a.n_tok || r >= a.m) continue;
-      const f32x4 sw = *(const f32x4 *)(a.w_scale + r);
-      const float sx = a.x_scale[t];
-      f32x4 y;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) y[e] = (float)v[e] * (sx * sw[e]);
-      float *dst = a.y + (size_t)t * a.m + r;
-      if (a.vec) {
-        *(f32x4 *)dst = y;
-      } else {
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-          if (r + e < a.m) dst[e] = y[e];
-      }
+      store_scaled(a, t, r, v, *(const f32x4 *)(a.w_scale + r));
     }
   }
+}
+
+// More token tiles: a wave owns NT weight tiles and all TT token tiles, the
+// kRingWaves waves of a workgroup kRingWaves NT weight tiles, and every fragment of
+// a stage -- KS k-steps of the workgroup's weights and activations -- is read once
+// per workgroup, by direct-to-LDS loads into a ring of three stages (two in flight
+// while one is multiplied).  grid: tile groups x K ranges; K range `split` of
+// several leaves its sums, 32-bit integers, in part[split][n_tok][16 tiles].
+constexpr int kRingWaves = 8, kRingMaxSplits = 8;
+typedef __attribute__((address_space(3))) void lds_void;
+
+template <int NT, int TT, int KS>
+__global__ __launch_bounds__(64 * kRingWaves) void k_linear_ring(LinearArgs a) {
+  constexpr int WT = kRingWaves * NT;      // weight tiles of a workgroup
+  constexpr int F = (WT + TT) * KS;        // fragments of a stage
+  constexpr int LPW = (F + kRingWaves - 1) / kRingWaves;  // of them per wave
+  __shared__ __attribute__((aligned(16))) char r0[LPW * kRingWaves * 1024],
+      r1[LPW * kRingWaves * 1024], r2[LPW * kRingWaves * 1024];
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int split = blockIdx.x % a.splits, tile0 = blockIdx.x / a.splits * WT;
+  const int tile_bytes = a.ks * 1024;
+  const int wn = min(WT, a.tiles - tile0);
+  const __amdgpu_buffer_rsrc_t wrs = uniform_rsrc(a.w + (size_t)tile0 * tile_bytes, wn * tile_bytes);
+  const __amdgpu_buffer_rsrc_t xrs = uniform_rsrc(a.x, a.ttiles * tile_bytes);
+  const int s0 = (int)((int64_t)a.ks * split / a.splits), s1 = (int)((int64_t)a.ks * (split + 1) / a.splits);
+  // Stage at k-step s into a buffer: fragment f is k-step f / (WT + TT), weight
+  // tile or token tile f % (WT + TT).  Steps past s1 and tiles past the last read
+  // zeros.
+  auto issue = [&](int s, char *dst) {
+#pragma unroll
+    for (int j = 0; j < LPW; ++j) {
+      const int f = w + j * kRingWaves;  // uniform
+      const int k = s + f / (WT + TT), t = f % (WT + TT);
+      const bool is_w = t < WT;
+      const bool in = f < F && k < s1 && (is_w ? t < wn : t - WT < a.ttiles);
+      const int at = ((is_w ? t : t - WT) * a.ks + k) * 1024 + lane * 16;
+      // (offsets: at most 16 tiles of 512 KB)
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(is_w ? wrs : xrs, (lds_void *)(dst + f * 1024), 16,
+                                               in ? at : 0x7fff0000, 0, 0, 0);
+    }
+  };
+  i32x4 acc[NT][TT];
+#pragma unroll
+  for (int i = 0; i < NT; ++i)
+#pragma unroll
+    for (int j = 0; j < TT; ++j) acc[i][j] = i32x4{0, 0, 0, 0};
+  issue(s0, r0);
+  issue(s0 + KS, r1);
+  // The stage at s is there once every wave has waited for its own loads of it
+  // (one later stage may be in flight) and met the others; then the buffer of the
+  // stage before is free.
+  auto round = [&](int s, const char *cur, char *nxt) {
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(LPW) : "memory");
+    issue(s + 2 * KS, nxt);
+    if (s >= s1) return;
+    const char *frag = cur + lane * 16;
+#pragma unroll
+    for (int k = 0; k < KS; ++k) {
+      i32x4 wf[NT];
+#pragma unroll
+      for (int i = 0; i < NT; ++i) wf[i] = *(const i32x4 *)(frag + (k * (WT + TT) + w * NT + i) * 1024);
+#pragma unroll
+      for (int j = 0; j < TT; ++j) {
+        const i32x4 xf = *(const i32x4 *)(frag + (k * (WT + TT) + WT + j) * 1024);
+#pragma unroll
+        for (int i = 0; i < NT; ++i) acc[i][j] = mfma16i(wf[i], xf, acc[i][j]);
+      }
+    }
+  };
+  for (int s = s0; s < s1; s += 3 * KS) {
+    round(s, r0, r2);
+    round(s + KS, r1, r0);
+    round(s + 2 * KS, r2, r1);
+  }
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // loads into LDS still in flight
+  // element e of lane l is channel 4 (l / 16) + e of the tile, token l % 16
+#pragma unroll
+  for (int i = 0; i < NT; ++i) {
+    const int r = (tile0 + w * NT + i) * 16 + 4 * (lane >> 4);
+    if (r >= a.tiles * 16) continue;
+    const f32x4 sw = *(const f32x4 *)(a.w_scale + r);
+#pragma unroll
+    for (int j = 0; j < TT; ++j) {
+      const int t = j * 16 + (lane & 15);
+      if (t >= a.n_tok) continue;
+      if (a.splits > 1) {
+        *(i32x4 *)(a.part + ((size_t)split * a.n_tok + t) * a.tiles * 16 + r) = acc[i][j];
+        continue;
+      }
+      store_scaled(a, t, r, acc[i][j], sw);
+    }
+  }
+}
+
+// The sums of the K ranges, scaled: four channels a thread.
+__global__ __launch_bounds__(256) void k_linear_join(LinearArgs a) {
+  const int quads = a.tiles * 4, i = blockIdx.x * 256 + threadIdx.x;
+  const int t = i / quads, r = (i - t * quads) * 4;
+  if (t >= a.n_tok) return;
+  const size_t stride = (size_t)a.n_tok * a.tiles * 16;
+  const int32_t *p = a.part + (size_t)t * a.tiles * 16 + r;
+  i32x4 v = *(const i32x4 *)p;
+  for (int k = 1; k < a.splits; ++k) v += *(const i32x4 *)(p + k * stride);
+  store_scaled(a, t, r, v, *(const f32x4 *)(a.w_scale + r));
 }
 
 template <int NT, int TT, int NW>
@@ -252,6 +366,82 @@ hipError_t launch_tt(const LinearArgs &a, int nt, hipStream_t s) {
     case 4: return launch_form<4, TT, TT <= 4 ? 8 : 4>(a, s);
     default: return hipErrorInvalidValue;
   }
+}
+
+template <int NT, int TT>
+hipError_t launch_ring(const LinearArgs &a, hipStream_t s) {
+  constexpr int KS = 48 / (kRingWaves * NT + TT);  // three stages of at most 48 KB
+  const int groups = ceil_div(a.tiles, kRingWaves * NT);
+  hipLaunchKernelGGL((k_linear_ring<NT, TT, KS>), dim3(groups * a.splits), dim3(64 * kRingWaves), 0,
+                     s, a);
+  if (a.splits > 1)
+    hipLaunchKernelGGL(k_linear_join, dim3(ceil_div(a.n_tok * a.tiles * 4, 256)), dim3(256), 0, s, a);
+  return hipGetLastError();
+}
+
+// Token tiles up to the next form: the multiplications of a tile that is not
+// there cost nothing next to the weights' bytes.
+template <int NT>
+hipError_t launch_ring_tt(const LinearArgs &a, hipStream_t s) {
+  if (NT == 1 && a.ttiles <= 2) return launch_ring<1, 2>(a, s);
+  if (NT == 1 && a.ttiles <= 3) return launch_ring<1, 3>(a, s);
+  if (a.ttiles <= 5) return launch_ring<NT, 5>(a, s);
+  if (a.ttiles <= 7) return launch_ring<NT, 7>(a, s);
+  if (a.ttiles <= 9) return launch_ring<NT, 9>(a, s);
+  if (a.ttiles <= 12) return launch_ring<NT, 12>(a, s);
+  return launch_ring<NT, 16>(a, s);
+}
+
+// Which of the two kernels, and with what: ring_tiles is 0 for k_linear with nt
+// weight tiles a workgroup and the token tiles in tblocks blocks, else the weight
+// tiles of a ring wave, over `splits` K ranges.
+struct LinearPlan {
+  int nt, tblocks, ring_tiles, splits;
+};
+
+// k_linear's workgroups read the activations once per weight tile group, the
+// ring's once per 128 or 256 channels, but the ring pays for its stages' barriers
+// and the join of K ranges, and needs a long stream.  Measured, k_linear / ring, us:
+//   rows                   17           33            65            129
+//   4096 x 4096         9.6 / 14.0  10.4 / 15.8   13.0 / 18.1   14.4 / -
+//   5120 x 5120        15.1 / 15.5  17.7 / 17.3   23.0 / 18.2
+//   22016 x 4096       24.1 / 24.7  26.9 / 26.6   32.6 / 28.7   43.7 / 34.4
+//   8192 x 8192        18.1 / 21.4  21.0 / 23.1   25.4 / 24.2
+//   8192 x 28672       51.6 / 53.9  60.9 / 56.7   76.5 / 61.7  100.3 / 75.1
+//   57344 x 8192       83.9 / 96.6  93.6 / 98.9  114.8 / 102.4 176.7 / 121.4
+//   10240 x 8192       26.9 / 24.9  31.9 / 26.0   39.2 / 27.9   50.0 / 34.7
+//   5120 x 13824       31.3 / 23.1  38.1 / 24.5   49.8 / 26.4   58.0 / 32.0
+// so the ring takes four or more token tiles of 24 MB of codes or more, and from
+// two on where k_linear leaves compute units idle in its last round of a long K
+// (the last two lines; on few rows k_linear is within a few percent of the stream).
+LinearPlan linear_plan(int tiles, int ks, int n_tok) {
+  LinearPlan p{};
+  const int ttiles = ceil_div(n_tok, 16);
+  p.splits = 1;
+  p.tblocks = ceil_div(ttiles, kLinearMaxTokenTiles);
+  // tiles per workgroup: as many (up to four) as leave a workgroup for every
+  // compute unit
+  p.nt = 4;
+  while (p.nt > 1 && ceil_div(tiles, p.nt) * p.tblocks < kAttnCUs) p.nt /= 2;
+  const int groups = ceil_div(tiles, p.nt), rounds = ceil_div(groups, kAttnCUs);
+  const int64_t bytes = (int64_t)tiles * ks * 1024;
+  const bool idle = ks >= 128 && bytes >= (64 << 20) && 4 * rounds * kAttnCUs > 5 * groups;
+  if (!(ttiles >= 4 && bytes >= (24 << 20)) && !(ttiles >= 2 && ttiles <= 3 && idle)) return p;
+  // 128 channels per workgroup; 256 where that leaves as few rounds of workgroups
+  // (57344 x 8192, 224 workgroups instead of 448), or for the most rows of a long K
+  // whose ranges still fill the compute units (256 rows: 8192 x 28672 110 -> 99 us,
+  // 10240 x 8192 56 -> 54; but 4096 x 11008 38 -> 42, 128 workgroups), as then the
+  // activations are read half as often
+  const int g1 = ceil_div(tiles, kRingWaves), g2 = ceil_div(tiles, 2 * kRingWaves);
+  const bool wide = g1 > kAttnCUs ? 2 * ceil_div(g2, kAttnCUs) <= ceil_div(g1, kAttnCUs)
+                                  : ttiles > 12 && ks >= 128 && g2 * kRingMaxSplits >= kAttnCUs;
+  p.ring_tiles = ttiles >= 4 && wide ? 2 : 1;
+  // K ranges of eight k-steps or more, up to a workgroup for every compute unit
+  p.splits = kAttnCUs / (p.ring_tiles == 2 ? g2 : g1);
+  if (p.splits > kRingMaxSplits) p.splits = kRingMaxSplits;
+  if (p.splits > ks / 8) p.splits = ks / 8;
+  if (p.splits < 1) p.splits = 1;
+  return p;
 }
 
 }  // namespace
@@ -297,25 +487,35 @@ hipError_t launch_quant_rows(const void *x, bool bf16, int n_tok, int k, uint8_t
   return hipGetLastError();
 }
 
-// Tiles per workgroup: as many (up to four) as leave a workgroup for every
-// compute unit.
+size_t linear_part_bytes(int m, int k, int max_rows) {
+  const LinearGeom g = linear_geom(m, k);
+  size_t most = 0;
+  for (int rows = max_rows; rows > 0; rows = round_up(rows, 16) - 16) {  // the most of each plan
+    const int splits = linear_plan(g.tiles, g.ks, rows).splits;
+    const size_t b = splits > 1 ? (size_t)splits * rows * g.tiles * 16 * sizeof(int32_t) : 0;
+    if (b > most) most = b;
+  }
+  return most;
+}
+
 hipError_t launch_linear(const LinearArgs &args, hipStream_t s) {
   LinearArgs a = args;
   a.vec = a.m % 4 == 0 && ((uintptr_t)a.y & 15) == 0;
   a.ttiles = ceil_div(a.n_tok, 16);
-  a.tblocks = ceil_div(a.ttiles, kLinearMaxTokenTiles);
-  const int tt = ceil_div(a.ttiles, a.tblocks);
-  int nt = 4;
-  while (nt > 1 && ceil_div(a.tiles, nt) * a.tblocks < kAttnCUs) nt /= 2;
-  switch (tt) {
-    case 1: return launch_tt<1>(a, nt, s);
-    case 2: return launch_tt<2>(a, nt, s);
-    case 3: return launch_tt<3>(a, nt, s);
-    case 4: return launch_tt<4>(a, nt, s);
-    case 5: return launch_tt<5>(a, nt, s);
-    case 6: return launch_tt<6>(a, nt, s);
-    case 7: return launch_tt<7>(a, nt, s);
-    case 8: return launch_tt<8>(a, nt, s);
+  const LinearPlan p = linear_plan(a.tiles, a.ks, a.n_tok);
+  a.tblocks = p.tblocks;
+  a.splits = p.splits;
+  if (p.ring_tiles == 1) return launch_ring_tt<1>(a, s);
+  if (p.ring_tiles == 2) return launch_ring_tt<2>(a, s);
+  switch (ceil_div(a.ttiles, a.tblocks)) {
+    case 1: return launch_tt<1>(a, p.nt, s);
+    case 2: return launch_tt<2>(a, p.nt, s);
+    case 3: return launch_tt<3>(a, p.nt, s);
+    case 4: return launch_tt<4>(a, p.nt, s);
+    case 5: return launch_tt<5>(a, p.nt, s);
+    case 6: return launch_tt<6>(a, p.nt, s);
+    case 7: return launch_tt<7>(a, p.nt, s);
+    case 8: return launch_tt<8>(a, p.nt, s);
     default: return hipErrorInvalidValue;
   }
 }

@@ -340,8 +340,11 @@ struct LinearArgs {
   const float *x_scale;
   float *y;  // [n_tok][m]
   int m, tiles, ks, n_tok;
-  int vec, ttiles, tblocks;  // filled in by the launch
+  int32_t *part;  // linear_part_bytes of them: the sums of K ranges
+  int vec, ttiles, tblocks, splits;  // filled in by the launch
 };
+// Bytes of the sums that a product of up to max_rows rows leaves for its join.
+size_t linear_part_bytes(int m, int k, int max_rows);
 hipError_t launch_linear(const LinearArgs &a, hipStream_t s);
 
 // What stands between the projections of an int8 model (k_int8.hip).

@@ -73,6 +73,61 @@ def test_linear(api, f32, m, k, n):
     assert np.array_equal(got, ref)
 
 
+@pytest.mark.parametrize("m,k,rows", [
+    (22005, 1160, (48, 49, 81, 97, 129, 180, 193, 256)),  # 128 channels a workgroup, whole K
+    (5003, 5128, (48, 64, 65, 130, 200, 256)),            # and six K ranges, the last channels' group short
+    (40001, 650, (49, 81, 98, 129, 177, 255)),            # 256 channels
+    (3001, 8200, (100, 193, 256)),                        # eight K ranges of 128 channels' groups
+    (8001, 8200, (193, 256)),                             # and of 256 channels'
+    (5120, 13130, (16, 17, 33, 47)),                      # a long K and an uneven split of the channels
+    (76810, 500, (50, 256)),                              # more workgroups than one round
+    (8200, 32768, (48, 60)),                              # the longest K, offsets of a tile group near 8 MB
+])
+def test_linear_large(api, m, k, rows):
+    """Matrices past 24 MB of codes: the workgroups share stages of both operands, and K ranges
+    of one product meet in the workspace.  Exact against the oracle on 400 channels, the first
+    and last among them; on a workspace sized for the most rows and full of other bytes."""
+    g = torch.Generator().manual_seed(m + k)
+    w = torch.randn((m, k), generator=g).bfloat16()
+    some = torch.cat([torch.arange(150), torch.randint(150, m - 150, (100,), generator=g), torch.arange(m - 150, m)])
+    packed = torch.full((api.sb_linear_packed_bytes(m, k),), 0x55, dtype=torch.uint8, device="cuda")
+    api.sb_linear_pack(w.cuda(), packed)
+    sizes = [api.sb_linear_workspace_bytes(m, k, n) for n in range(1, 257)]
+    assert sizes == sorted(sizes)
+    ws = torch.full((sizes[rows[-1] - 1],), 0xff, dtype=torch.uint8, device="cuda")
+    wf = w[some].float().numpy()
+    for n in rows:
+        say("large linear", m, k, n)
+        x = torch.randn((n, k), generator=g).bfloat16()
+        buf = torch.full((n * m + 64,), 7.0, device="cuda")
+        y = buf[:n * m].view(n, m)
+        api.sb_linear_quantized(packed, x.cuda(), y, ws)
+        assert (buf[n * m:] == 7.0).all()
+        assert np.array_equal(y[:, some.cuda()].cpu().numpy(), int8.linear(x.float().numpy(), wf))
+
+
+def test_linear_large_captured(api):
+    """K ranges and their join in a graph, beside eager calls on a workspace of their own."""
+    m, k, n = 5003, 5128, 70
+    g = torch.Generator().manual_seed(5)
+    packed = torch.empty(api.sb_linear_packed_bytes(m, k), dtype=torch.uint8, device="cuda")
+    api.sb_linear_pack(torch.randn((m, k), generator=g).bfloat16().cuda(), packed)
+    x0 = torch.randn((n, k), generator=g).cuda()
+    xd, y, y2 = x0.clone(), torch.zeros((n, m), device="cuda"), torch.zeros((n, m), device="cuda")
+    ws, ws2 = (torch.empty(api.sb_linear_workspace_bytes(m, k, n), dtype=torch.uint8, device="cuda") for _ in range(2))
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        api.sb_linear_quantized(packed, xd, y, ws)
+    for i in range(4):
+        xd.copy_(x0 * (3.0 if i % 2 else -1.0) + i)
+        y.zero_()
+        graph.replay()
+        api.sb_linear_quantized(packed, xd, y2, ws2)
+        torch.cuda.synchronize()
+        assert torch.equal(y, y2) and y.abs().max() > 0
+
+
 def test_linear_special_rows(api):
     """Zero rows and channels, NaN and infinity in one: they stay where they are."""
     g = np.random.default_rng(1)
