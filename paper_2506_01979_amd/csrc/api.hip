@@ -1772,10 +1772,10 @@ sb_status sb_count_step(int32_t vocab, int32_t n_rows, const int32_t *d_tokens,
 
 size_t sb_shape_workspace_bytes(int32_t vocab, int32_t n_rows) {
   if (vocab < 1 || vocab > SB_BRANCH_MAX_VOCAB || n_rows < 1 || n_rows > SB_MAX_ROWS) return 0;
-  // every smaller tree may take the finer slices of few rows
+  // smaller trees may take the finer slices of few rows, 4096 at most
   const size_t here = (size_t)shape_groups(vocab, n_rows) * n_rows;
-  const size_t fewer = shape_groups(vocab, 1) == shape_groups(vocab, n_rows) ? here : 1024;
-  return align_up((here > fewer ? here : fewer) * sizeof(LmPart));
+  const size_t fewer = shape_groups(vocab, 1) == shape_groups(vocab, n_rows) ? here : 4096;
+  return align_up((here > fewer ? here : fewer) * sizeof(LmPart)) + align_up(shape_path_bytes(n_rows));
 }
 
 sb_status sb_shape_logits(int32_t vocab, int32_t n_rows, const sb_logit_rules *rules,
@@ -1798,6 +1798,7 @@ sb_status sb_shape_logits(int32_t vocab, int32_t n_rows, const sb_logit_rules *r
   const bool rep = r.repetition != 1.0f, pen = rep || r.presence != 0.0f || r.frequency != 0.0f;
   ShapeArgs a{};
   a.vocab = vocab;
+  a.n_rows = n_rows;
   a.logits = d_logits;
   a.out = d_out;
   a.prompt = rep ? r.d_prompt : nullptr;
@@ -1806,6 +1807,7 @@ sb_status sb_shape_logits(int32_t vocab, int32_t n_rows, const sb_logit_rules *r
   a.mask = r.d_mask;
   a.mask_stride = r.mask_stride;
   a.repetition = r.repetition;
+  a.inv_repetition = r.repetition >= 0x1p-20f && r.repetition <= 0x1p+20f ? 1.0f / r.repetition : NAN;
   a.presence = r.presence;
   a.frequency = r.frequency;
   a.tokens = d_tokens;
@@ -1813,7 +1815,8 @@ sb_status sb_shape_logits(int32_t vocab, int32_t n_rows, const sb_logit_rules *r
   a.greedy = temperature <= 0.0f ? 1 : 0;
   a.inv_t = a.greedy ? 1.0f : 1.0f / temperature;
   a.part = (LmPart *)d_ws;
-  SB_TRY(launch_shape_logits(a, tree, n_rows, stream));
+  a.paths = (uint64_t *)((char *)d_ws + align_up((size_t)shape_groups(vocab, n_rows) * n_rows * sizeof(LmPart)));
+  SB_TRY(launch_shape_logits(a, tree, stream));
   return hip_status(launch_stats_finish(a.part, shape_groups(vocab, n_rows), n_rows, temperature,
                                         d_stats, stream, true));
 }

@@ -68,104 +68,243 @@ __global__ __launch_bounds__(SB_MAX_ROWS) void k_count_step(int vocab, int n_row
   if (tok >= 0 && tok < vocab) atomicAdd(&counts[tok], 1);
 }
 
-__device__ __forceinline__ double wave_sum(double v) {
-  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
+// A value of every lane joined over the wave: pairs, quads, half rows and rows of
+// 16 by DPP, then the four rows.  Every lane returns the same value.
+template <int kCtrl, typename T>
+__device__ __forceinline__ T dpp(T v) {
+  uint32_t b[sizeof(T) / 4];
+  __builtin_memcpy(b, &v, sizeof(T));
+#pragma unroll
+  for (uint32_t &x : b) x = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, kCtrl, 0xf, 0xf, false);
+  __builtin_memcpy(&v, b, sizeof(T));
   return v;
 }
+template <typename T>
+__device__ __forceinline__ T read_lane(T v, int l) {
+  uint32_t b[sizeof(T) / 4];
+  __builtin_memcpy(b, &v, sizeof(T));
+#pragma unroll
+  for (uint32_t &x : b) x = (uint32_t)__builtin_amdgcn_readlane((int)x, l);
+  __builtin_memcpy(&v, b, sizeof(T));
+  return v;
+}
+template <typename T, typename Op>
+__device__ __forceinline__ T wave_join(T v, Op op) {
+  v = op(v, dpp<0xB1>(v));   // quad_perm [1,0,3,2]
+  v = op(v, dpp<0x4E>(v));   // quad_perm [2,3,0,1]
+  v = op(v, dpp<0x141>(v));  // row_half_mirror
+  v = op(v, dpp<0x140>(v));  // row_mirror
+  return op(op(read_lane(v, 0), read_lane(v, 16)), op(read_lane(v, 32), read_lane(v, 48)));
+}
 
-// Rows x slices of kT E tokens.  VEC: 16-byte accesses (vocab % 4 == 0 and
-// every row and array 16-byte aligned), a thread's tokens in fours; otherwise
-// one by one along the slice.  The slice's part of the statistics goes to
-// part[row][slice] as the LM head's epilogue leaves it (LmPart).
-template <int E, bool VEC>
-__global__ __launch_bounds__(kT) void k_shape_logits(ShapeArgs a, TreeArg tree) {
-  constexpr int kSpan = kT * E;
+// LDS that one wave writes and reads: its operations stay in order.
+__device__ __forceinline__ void wave_sync() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+
+// y / d, correctly rounded, for quotients that `plain` says.  r is 1 / d correctly
+// rounded, NaN for d outside [2^-20, 2^20]: y r is then within 1.5 ulp of the
+// quotient, one exact residual brings it within one, and from there the next gives
+// the rounded quotient (Markstein, 1990).  Quotients below 2^-60 or above 2^100 may
+// leave inexact residuals; the compiler's division has about twice the instructions.
+__device__ __forceinline__ float quotient(float y, float d, float r) {
+  const float q0 = y * r;
+  const float q1 = fmaf(fmaf(-q0, d, y), r, q0);
+  return fmaf(fmaf(-q1, d, y), r, q1);
+}
+__device__ __forceinline__ bool plain(float y, float r) {
+  return __float_as_uint(y * r) - 0x21800000u < 0x71800000u - 0x21800000u;
+}
+
+// e^t for t <= 0 (any t below -200 or NaN: about e^-200): 2^p by the hardware, 1
+// ulp, with p = t log2(e) rounded and what it leaves put back.
+__device__ __forceinline__ float exp_below(float t) {
+  t = fmaxf(t, -200.0f);
+  const float p = t * 0x1.715476p+0f;
+  const float rest = fmaf(t, 0x1.4ae0cp-26f, fmaf(t, 0x1.715476p+0f, -p));
+  const float e = __builtin_amdgcn_exp2f(p);
+  return fmaf(e, rest * 0x1.62e43p-1f, e);
+}
+
+// The drafts on every row's path (its ancestors and itself, the root aside), as
+// bits: of up to 128 rows an argument of the kernel (2 KB of the 4 that arguments
+// have), of larger trees left in the workspace by k_tree_paths.
+constexpr int kPathArgRows = 128;
+struct PathMasks {
+  uint64_t on[kPathArgRows][2];
+};
+
+// Row i: each round joins the path of the row that the jump leads to, then the
+// jumps double.
+__global__ __launch_bounds__(SB_MAX_ROWS) void k_tree_paths(TreeArg tree, uint64_t *paths) {
   __shared__ int16_t s_jump[SB_MAX_ROWS];
-  __shared__ uint8_t s_on[SB_MAX_ROWS];
-  __shared__ int s_cnt[kSpan];
-  __shared__ float s_best[kT / 64];
-  __shared__ int s_arg[kT / 64], s_bad[kT / 64];
-  __shared__ double s_sum[kT / 64];
-  const int row = blockIdx.y, v0 = blockIdx.x * kSpan, tid = threadIdx.x;
-  const float *l = a.logits + (size_t)row * a.vocab;
-  float *out = a.out + (size_t)row * a.vocab;
-  const uint32_t *mask = a.mask ? a.mask + (size_t)row * a.mask_stride : nullptr;
-  // token of element e of this thread
-  auto token = [&](int e) { return VEC ? v0 + 4 * (tid + kT * (e >> 2)) + (e & 3) : v0 + tid + kT * e; };
-  // every load before the first use; tokens past the vocabulary read as zeros
-  float x[E], bias[E];
-  int c[E], pr[E];
-  uint32_t mw[E];
-  auto load = [&](const auto *p, auto (&d)[E], bool there) {
+  __shared__ uint64_t s_on[SB_MAX_ROWS][4];
+  const int i = threadIdx.x;
+  uint64_t on[4];
+  int jump = i < tree.n ? tree.parent[i] : -1;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) on[k] = i > 0 && i >> 6 == k ? 1ull << (i & 63) : 0;
+  for (int step = 1; step < tree.n; step <<= 1) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) s_on[i][k] = on[k];
+    s_jump[i] = (int16_t)jump;
+    __syncthreads();
+    if (jump >= 0) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) on[k] |= s_on[jump][k];
+      jump = s_jump[jump];
+    }
+    __syncthreads();
+  }
+  if (i < tree.n) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) paths[i * 4 + k] = on[k];
+  }
+}
+
+// A wave owns a slice of 64 E tokens of a row and shares nothing with others: no
+// barriers, and the finishing pass joins the slices.  VEC: 16-byte accesses (vocab %
+// 4 == 0 and every row and array 16-byte aligned), a lane's tokens in fours;
+// otherwise one by one along the slice.  The slice's part of the statistics goes to
+// part[row][slice] as the LM head's epilogue leaves it (LmPart).
+//
+// Bound by the logits' way in and out and by the vector unit: 37 rows of 128256
+// under every rule are 38 MB of them, 8 us at a copy's rate, and some 45 instructions
+// per token; 11 us and the finishing pass's 4.  Tried and not kept: slices of a
+// workgroup with barriers between its waves (14.5), 16 tokens a lane (more registers,
+// 0.3 to 1.5 us slower), several rows per wave with the counts read once (the same or
+// slower), the penalties on a compacted list of seen tokens (the same at 37 rows,
+// slower above).
+template <int E, bool VEC>
+__global__ __launch_bounds__(kT) void k_shape_logits(ShapeArgs a, PathMasks paths) {
+  constexpr int kSlice = 64 * E;
+  __shared__ int s_cnt[kT / 64][kSlice];
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int slice = blockIdx.x * (kT / 64) + w, v0 = slice * kSlice, row = blockIdx.y;
+  if (slice >= a.groups) return;
+  // place in the slice, and token, of element e of this lane
+  auto place = [&](int e) { return VEC ? 4 * (lane + 64 * (e >> 2)) + (e & 3) : lane + 64 * e; };
+  auto token = [&](int e) { return v0 + place(e); };
+  // every load before the first use; tokens past the vocabulary read as zeros and
+  // are not allowed, which keeps them out of the statistics
+  auto load = [&](const auto *p, auto (&d)[E]) {
     typedef decltype(d[0] + d[0]) T;
     typedef T V4 __attribute__((ext_vector_type(4)));
     if (VEC) {
 #pragma unroll
       for (int e = 0; e < E; e += 4) {
-        const V4 t = there && token(e) < a.vocab ? *(const V4 *)(p + token(e)) : V4{0, 0, 0, 0};
+        const V4 t = p && token(e) < a.vocab ? *(const V4 *)(p + token(e)) : V4{0, 0, 0, 0};
 #pragma unroll
         for (int i = 0; i < 4; ++i) d[e + i] = t[i];
       }
     } else {
 #pragma unroll
-      for (int e = 0; e < E; ++e) d[e] = there && token(e) < a.vocab ? p[token(e)] : (T)0;
+      for (int e = 0; e < E; ++e) d[e] = p && token(e) < a.vocab ? p[token(e)] : (T)0;
     }
   };
-  load(l, x, true);
-  load(a.output, c, a.output != nullptr);
-  load(a.prompt, pr, a.prompt != nullptr);
-  load(a.bias, bias, a.bias != nullptr);
+  // the tree's tokens on the row's path: tree row lane + 64 k
+  constexpr int kTok = SB_MAX_ROWS / 64;
+  int tok[kTok];
+  uint64_t on[kTok];
+#pragma unroll
+  for (int k = 0; k < kTok; ++k) {
+    tok[k] = a.count_drafts && lane + 64 * k < a.n_rows ? a.tokens[lane + 64 * k] : -1;
+    on[k] = a.count_drafts && 64 * k < a.n_rows ? (a.paths ? a.paths[row * 4 + k] : paths.on[row][k & 1]) : 0;
+  }
+  float x[E], bias[E];
+  int c[E], pr[E];
+  uint32_t allowed[VEC ? E / 4 : E];
+  load(a.output, c);
+  load(a.prompt, pr);
+  load(a.logits + (size_t)row * a.vocab, x);
+  load(a.bias, bias);
+  const uint32_t *mask = a.mask ? a.mask + (size_t)row * a.mask_stride : nullptr;
 #pragma unroll
   for (int e = 0; e < E; e += VEC ? 4 : 1)
-    mw[e] = mask && token(e) < a.vocab ? mask[token(e) >> 5] : ~0u;
+    allowed[VEC ? e / 4 : e] = token(e) < a.vocab ? (mask ? mask[token(e) >> 5] : ~0u) : 0u;
 
-  // ---- the row's drafts in this slice.  Round r marks the 2^r-th ancestors of
-  // the rows marked so far, then all jumps double.
-  int drafts = 0;
+  // ---- the drafts on the row's path in this slice
+  bool drafts = false;
   if (a.count_drafts) {
-    const int tok = tid >= 1 && tid < tree.n ? a.tokens[tid] : -1;
-    int jump = tid < tree.n ? tree.parent[tid] : -1;
-    s_jump[tid] = (int16_t)jump;
-    s_on[tid] = tid == row;
+    bool mine[kTok];
 #pragma unroll
-    for (int e = 0; e < E; ++e) s_cnt[tid + kT * e] = 0;
-    __syncthreads();
-    for (int step = 1; step < tree.n; step <<= 1) {
-      const int next = jump >= 0 ? s_jump[jump] : -1;
-      if (jump >= 0 && s_on[tid]) s_on[jump] = 1;
-      __syncthreads();
-      jump = next;
-      s_jump[tid] = (int16_t)next;
-      __syncthreads();
+    for (int k = 0; k < kTok; ++k) {
+      mine[k] = (on[k] >> lane & 1) && tok[k] >= v0 && tok[k] < a.vocab && tok[k] - v0 < kSlice;
+      drafts |= mine[k];
     }
-    const bool mine = s_on[tid] && tok >= v0 && tok < a.vocab && tok - v0 < kSpan;
-    if (mine) atomicAdd(&s_cnt[tok - v0], 1);
-    drafts = __syncthreads_or(mine);
+    drafts = __any(drafts);
+    if (drafts) {
+#pragma unroll
+      for (int e = 0; e < E; ++e) s_cnt[w][lane + 64 * e] = 0;
+      wave_sync();
+#pragma unroll
+      for (int k = 0; k < kTok; ++k)
+        if (mine[k]) atomicAdd(&s_cnt[w][tok[k] - v0], 1);
+      wave_sync();
+    }
   }
 
-  // ---- the rules
-  float best = -INFINITY;
-  int arg = INT_MAX, bad = 0;
+  // ---- the penalties
+  if (a.output || a.prompt || drafts) {
+    if (drafts) {
 #pragma unroll
-  for (int e = 0; e < E; ++e) {
-    const int v = token(e);
-    float y = x[e];
-    const int ci = c[e] + (drafts ? s_cnt[v - v0] : 0);
-    const float cf = (float)ci;
-    if (ci > 0 || pr[e] > 0) y = y > 0.0f ? y / a.repetition : y * a.repetition;
-    y = y - a.frequency * cf;
-    if (ci > 0) y = y - a.presence;
-    if (a.bias) y = y + bias[e];
-    if (!((mw[VEC ? e & ~3 : e] >> (v & 31)) & 1u)) y = -INFINITY;
-    x[e] = y;
-    if (v < a.vocab) {
-      if (isnan(y) || y == INFINITY) bad = 1;
-      if (y > best || (y == best && v < arg && y > -INFINITY)) {
-        best = y;
-        arg = v;
+      for (int e = 0; e < E; ++e) c[e] += s_cnt[w][place(e)];
+    }
+    if (a.repetition != 1.0f) {
+      bool slow = false;
+#pragma unroll
+      for (int e = 0; e < E; ++e) slow |= (x[e] > 0.0f) & !plain(x[e], a.inv_repetition);
+      if (__any(slow)) {
+#pragma unroll 1
+        for (int e = 0; e < E; ++e) {
+          // one element a turn, in place of element 0: this is rare, and unrolled it
+          // would be most of the kernel
+          if (max(c[0], pr[0]) > 0) x[0] = x[0] > 0.0f ? x[0] / a.repetition : x[0] * a.repetition;
+          const float x0 = x[0];
+          const int c0 = c[0], p0 = pr[0];
+#pragma unroll
+          for (int k = 0; k + 1 < E; ++k) {
+            x[k] = x[k + 1];
+            c[k] = c[k + 1];
+            pr[k] = pr[k + 1];
+          }
+          x[E - 1] = x0;
+          c[E - 1] = c0;
+          pr[E - 1] = p0;
+        }
+      } else {
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+          const float q = quotient(x[e], a.repetition, a.inv_repetition), p = x[e] * a.repetition;
+          const float z = x[e] > 0.0f ? q : p;
+          x[e] = max(c[e], pr[e]) > 0 ? z : x[e];
+        }
       }
     }
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      x[e] = x[e] - a.frequency * (float)c[e];
+      x[e] = x[e] - (c[e] > 0 ? a.presence : 0.0f);
+    }
   }
+
+  // ---- bias and mask
+  if (a.bias) {
+#pragma unroll
+    for (int e = 0; e < E; ++e) x[e] = x[e] + bias[e];
+  }
+  float best = -INFINITY;
+  bool bad = false;
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    const uint32_t bit = VEC ? (allowed[e >> 2] >> (token(e & ~3) & 31)) & (1u << (e & 3))
+                             : (allowed[e] >> (token(e) & 31)) & 1u;
+    x[e] = bit ? x[e] : -INFINITY;
+    bad |= !(x[e] < INFINITY);  // NaN or +inf
+    best = fmaxf(best, x[e]);
+  }
+  float *out = a.out + (size_t)row * a.vocab;
   if (VEC) {
 #pragma unroll
     for (int e = 0; e < E; e += 4)
@@ -177,79 +316,71 @@ __global__ __launch_bounds__(kT) void k_shape_logits(ShapeArgs a, TreeArg tree) 
   }
 
   // ---- the slice's part of the statistics
-  const int lane = tid & 63, w = tid >> 6;
-  for (int o = 32; o > 0; o >>= 1) {
-    const float ob = __shfl_xor(best, o, 64);
-    const int oa = __shfl_xor(arg, o, 64);
-    if (ob > best || (ob == best && oa < arg)) {
-      best = ob;
-      arg = oa;
-    }
-    bad |= __shfl_xor(bad, o, 64);
-  }
-  if (lane == 0) {
-    s_best[w] = best;
-    s_arg[w] = arg;
-    s_bad[w] = bad;
-  }
-  __syncthreads();
-  best = s_best[0];
-  arg = s_arg[0];
-  bad = s_bad[0];
+  best = wave_join(best, [](float p, float q) { return fmaxf(p, q); });
+  int arg = INT_MAX;  // the first token of the maximum
 #pragma unroll
-  for (int k = 1; k < kT / 64; ++k) {
-    if (s_best[k] > best || (s_best[k] == best && s_arg[k] < arg)) {
-      best = s_best[k];
-      arg = s_arg[k];
-    }
-    bad |= s_bad[k];
-  }
+  for (int e = E - 1; e >= 0; --e) arg = x[e] == best ? token(e) : arg;
+  arg = wave_join(arg, [](int p, int q) { return min(p, q); });
   double sum = 0.0;
   if (!a.greedy) {
-    const float m = best == -INFINITY ? 0.0f : best * a.inv_t;
+    float m = best * a.inv_t;  // past float32 also from a finite best
+    if (m == -INFINITY) m = 0.0f;
+    bad |= m == INFINITY;  // z - m is of two infinities
 #pragma unroll
-    for (int e = 0; e < E; ++e) {
-      const float z = x[e] * a.inv_t;
-      if (token(e) < a.vocab) sum += (double)expf(z - m);
-    }
-    sum = wave_sum(sum);
-    if (lane == 0) s_sum[w] = sum;
-    __syncthreads();
-    sum = (s_sum[0] + s_sum[1]) + (s_sum[2] + s_sum[3]);
+    for (int e = 0; e < E; ++e) sum += (double)exp_below(x[e] * a.inv_t - m);
+    sum = wave_join(sum, [](double p, double q) { return p + q; });
   }
-  if (tid == 0)
-    a.part[(size_t)row * gridDim.x + blockIdx.x] = LmPart{best, arg, bad ? (double)NAN : sum};
+  bad = __any(bad);
+  if (lane == 0)
+    a.part[(size_t)row * a.groups + slice] =
+        LmPart{best, best == -INFINITY ? INT_MAX : arg, bad ? (double)NAN : sum};
 }
 
-// Tokens per thread: 4 while the launch then has at most four workgroups per
-// compute unit and the finishing pass's 256 slices hold the vocabulary.
+// Tokens per lane: 4 while the launch then has at most four workgroups per compute
+// unit and the slices are at most 512 (1 row of 32000: 5.4 us with 4, 5.9 with 8).
 int shape_e(int vocab, int n_rows) {
-  const int64_t g4 = (vocab + kT * 4 - 1) / (kT * 4);
-  return g4 <= 256 && g4 * n_rows <= 1024 ? 4 : 16;
+  const int64_t g4 = (vocab + 255) / 256;
+  return g4 <= 512 && g4 * n_rows <= 4096 ? 4 : 8;
 }
 
 }  // namespace
 
 int shape_groups(int vocab, int n_rows) {
-  const int span = kT * shape_e(vocab, n_rows);
-  return (vocab + span - 1) / span;
+  const int slice = 64 * shape_e(vocab, n_rows);
+  return (vocab + slice - 1) / slice;
 }
 
-hipError_t launch_shape_logits(const ShapeArgs &a, const TreeArg &tree, int n_rows, hipStream_t s) {
-  const dim3 grid(shape_groups(a.vocab, n_rows), n_rows);
+size_t shape_path_bytes(int n_rows) {
+  return n_rows > kPathArgRows ? (size_t)n_rows * 4 * sizeof(uint64_t) : 0;
+}
+
+hipError_t launch_shape_logits(const ShapeArgs &args, const TreeArg &tree, hipStream_t s) {
+  ShapeArgs a = args;
+  const int n = a.n_rows;
+  a.groups = shape_groups(a.vocab, n);
+  PathMasks paths;
+  if (!a.count_drafts || n <= kPathArgRows) {
+    a.paths = nullptr;
+    for (int i = 0; a.count_drafts && i < n; ++i)  // a parent's row comes before its children's
+      for (int k = 0; k < 2; ++k)
+        paths.on[i][k] = i > 0 ? paths.on[tree.parent[i]][k] | (i >> 6 == k ? 1ull << (i & 63) : 0) : 0;
+  } else {
+    hipLaunchKernelGGL(k_tree_paths, dim3(1), dim3(SB_MAX_ROWS), 0, s, tree, a.paths);
+  }
   const uintptr_t at = (uintptr_t)a.logits | (uintptr_t)a.out | (uintptr_t)a.output |
                        (uintptr_t)a.prompt | (uintptr_t)a.bias;
   const bool vec = a.vocab % 4 == 0 && (at & 15) == 0;
-  if (shape_e(a.vocab, n_rows) == 4) {
+  const dim3 grid((a.groups + kT / 64 - 1) / (kT / 64), n);
+  if (shape_e(a.vocab, n) == 4) {
     if (vec)
-      hipLaunchKernelGGL((k_shape_logits<4, true>), grid, dim3(kT), 0, s, a, tree);
+      hipLaunchKernelGGL((k_shape_logits<4, true>), grid, dim3(kT), 0, s, a, paths);
     else
-      hipLaunchKernelGGL((k_shape_logits<4, false>), grid, dim3(kT), 0, s, a, tree);
+      hipLaunchKernelGGL((k_shape_logits<4, false>), grid, dim3(kT), 0, s, a, paths);
   } else {
     if (vec)
-      hipLaunchKernelGGL((k_shape_logits<16, true>), grid, dim3(kT), 0, s, a, tree);
+      hipLaunchKernelGGL((k_shape_logits<8, true>), grid, dim3(kT), 0, s, a, paths);
     else
-      hipLaunchKernelGGL((k_shape_logits<16, false>), grid, dim3(kT), 0, s, a, tree);
+      hipLaunchKernelGGL((k_shape_logits<8, false>), grid, dim3(kT), 0, s, a, paths);
   }
   return hipGetLastError();
 }

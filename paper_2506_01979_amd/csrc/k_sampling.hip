@@ -181,6 +181,13 @@ __global__ __launch_bounds__(256) void k_softmax_stats_finish(const LmPart *__re
   if ((int)threadIdx.x < groups) p = part[(size_t)blockIdx.x * groups + threadIdx.x];
   float best = p.lmax;
   int arg = p.arg;
+  for (int i = threadIdx.x + 256; i < groups; i += 256) {
+    const LmPart r = part[(size_t)blockIdx.x * groups + i];
+    if (r.lmax > best || (r.lmax == best && r.arg < arg)) {
+      best = r.lmax;
+      arg = r.arg;
+    }
+  }
   for (int o = 32; o > 0; o >>= 1) {
     const float ob = __shfl_xor(best, o, 64);
     const int oa = __shfl_xor(arg, o, 64);
@@ -204,6 +211,10 @@ __global__ __launch_bounds__(256) void k_softmax_stats_finish(const LmPart *__re
   const float zmax = greedy ? best : best * inv_t;
   double term = p.sum;
   if (!greedy && p.sum != 0.0) term = p.sum * exp((double)(p.lmax * inv_t) - (double)zmax);
+  for (int i = threadIdx.x + 256; i < groups; i += 256) {
+    const LmPart r = part[(size_t)blockIdx.x * groups + i];
+    term += !greedy && r.sum != 0.0 ? r.sum * exp((double)(r.lmax * inv_t) - (double)zmax) : r.sum;
+  }
   const double s = block_sum<NW>(term, red);
   if (threadIdx.x == 0) {
     sb_row_stats st;
@@ -212,7 +223,7 @@ __global__ __launch_bounds__(256) void k_softmax_stats_finish(const LmPart *__re
     if (greedy)
       st.total = isnan(s) || (masked && best == -INFINITY) ? (double)NAN : 1.0;
     else
-      st.total = best == -INFINITY ? (double)NAN : s;
+      st.total = zmax == -INFINITY ? (double)NAN : s;
     out[blockIdx.x] = st;
   }
 }
@@ -597,7 +608,7 @@ hipError_t launch_softmax_stats(int vocab, int n_rows, const float *logits, floa
 
 hipError_t launch_stats_finish(const LmPart *part, int groups, int n_rows, float temperature,
                                sb_row_stats *stats, hipStream_t s, bool masked) {
-  if (groups < 1 || groups > 256 || n_rows < 1) return hipErrorInvalidValue;
+  if (groups < 1 || n_rows < 1) return hipErrorInvalidValue;
   float inv_t;
   int greedy;
   temp_args(temperature, &inv_t, &greedy);

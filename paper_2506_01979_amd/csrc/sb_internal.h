@@ -31,13 +31,14 @@ struct LmPart {
   double sum;
 };
 // One row per workgroup: the statistics of rows 0 .. n_rows - 1 from their
-// groups' partials, part[row][groups] (at most 256 groups).  masked: a row
+// groups' partials, part[row][groups].  masked: a row
 // with nothing above -inf has NaN total at T = 0 too.
 hipError_t launch_stats_finish(const LmPart *part, int groups, int n_rows, float temperature,
                                sb_row_stats *stats, hipStream_t s, bool masked = false);
 // ---- counts and rules on logits (k_logits.hip) ------------------------------
 struct ShapeArgs {
-  int vocab;
+  int vocab, n_rows;
+  int groups;  // filled in by the launch
   const float *logits;
   float *out;
   const int32_t *prompt, *output;  // nullable, as below
@@ -45,14 +46,17 @@ struct ShapeArgs {
   const uint32_t *mask;
   int mask_stride;
   float repetition, presence, frequency;
+  float inv_repetition;  // 1 / repetition for one in [2^-20, 2^20], else NaN
   const int32_t *tokens;
   int count_drafts;  // the drafts on a row's path count
   float inv_t;
   int greedy;
   LmPart *part;  // [n_rows][shape_groups]
+  uint64_t *paths;  // shape_path_bytes
 };
+size_t shape_path_bytes(int n_rows);
 int shape_groups(int vocab, int n_rows);
-hipError_t launch_shape_logits(const ShapeArgs &a, const TreeArg &tree, int n_rows, hipStream_t s);
+hipError_t launch_shape_logits(const ShapeArgs &a, const TreeArg &tree, hipStream_t s);
 hipError_t launch_count_tokens(int vocab, int n, const int32_t *tokens, int accumulate,
                                int32_t *counts, hipStream_t s);
 hipError_t launch_count_step(int vocab, int n_rows, const int32_t *tokens,
