@@ -263,15 +263,16 @@ def _host_i32(a) -> tuple:
     return arr, C.byref(C.c_int32.from_address(arr.__array_interface__["data"][0]))
 
 
-def _on_stream_device(stream, *tensors) -> None:
-    """The tensors' device is the stream's and the current one: a launch goes
-    to the current device, where another's memory would fault."""
-    cur = torch.cuda.current_device()
-    if stream is not None and stream.device.index != cur:
-        raise ValueError(f"the stream is on device {stream.device.index}, the current one is {cur}")
+def _stream_on(stream, *tensors) -> int:
+    """The launch's stream, whose device and the tensors' is the current one: a
+    launch goes to the current device, where another's memory would fault."""
+    cur = torch._C._cuda_getDevice()
+    if stream is not None and stream.device_index != cur:
+        raise ValueError(f"the stream is on device {stream.device_index}, the current one is {cur}")
     for t in tensors:
-        if t is not None and t.device.index != cur:
+        if t is not None and t.get_device() != cur:
             raise ValueError(f"a tensor is on {t.device}, the current device is {cur}")
+    return torch._C._cuda_getCurrentRawStream(cur) if stream is None else stream.cuda_stream
 
 
 def make_config(shape, projections=None) -> ModelConfig:
@@ -535,7 +536,7 @@ class QuantizedKV:
         c = self.cfg
         if (cfg.n_layers, cfg.n_kv_heads, cfg.head_dim) != (c.n_layers, c.n_kv_heads, c.head_dim):
             raise ValueError("the cache was made for another n_layers, n_kv_heads or head_dim")
-        _on_stream_device(stream, self.k, *tensors)
+        _stream_on(stream, self.k, *tensors)
         return C.byref(self._struct)
 
 
@@ -594,8 +595,8 @@ def sb_linear_pack(w: torch.Tensor, packed: torch.Tensor, stream=None) -> None:
     m, k = w.shape
     _need(w, 0, "w", torch.bfloat16)
     _need(packed, sb_linear_packed_bytes(m, k), "packed")
-    _on_stream_device(stream, w, packed)
-    _check(lib.sb_linear_pack(m, k, w.data_ptr(), packed.data_ptr(), _stream(stream)),
+    handle = _stream_on(stream, w, packed)
+    _check(lib.sb_linear_pack(m, k, w.data_ptr(), packed.data_ptr(), handle),
            "sb_linear_pack")
 
 
@@ -620,10 +621,10 @@ def sb_linear_quantized(packed: torch.Tensor, x: torch.Tensor, y: torch.Tensor, 
         raise ValueError(f"packed: {packed.nbytes} bytes, a [{m}][{k}] matrix has {need}")
     _need(packed, need, "packed")
     _need(ws, 0, "ws")
-    _on_stream_device(stream, packed, x, y, ws)
+    handle = _stream_on(stream, packed, x, y, ws)
     _check(lib.sb_linear_quantized(m, k, packed.data_ptr(), n, x.data_ptr(),
                                    SB_BF16 if x.dtype is torch.bfloat16 else SB_F32, y.data_ptr(),
-                                   ws.data_ptr(), ws.nbytes, _stream(stream)),
+                                   ws.data_ptr(), ws.nbytes, handle),
            "sb_linear_quantized")
 
 
@@ -632,9 +633,9 @@ def sb_count_tokens(tokens: torch.Tensor, counts: torch.Tensor, accumulate: bool
     """tokens int32 [n]; counts int32 [vocab]."""
     _need(tokens, 0, "tokens", torch.int32)
     _need(counts, 0, "counts", torch.int32)
-    _on_stream_device(stream, tokens, counts)
+    handle = _stream_on(stream, tokens, counts)
     _check(lib.sb_count_tokens(counts.numel(), tokens.numel(), tokens.data_ptr(), int(accumulate),
-                               counts.data_ptr(), _stream(stream)), "sb_count_tokens")
+                               counts.data_ptr(), handle), "sb_count_tokens")
 
 
 def sb_count_step(tokens: torch.Tensor, result: torch.Tensor, counts: torch.Tensor,
@@ -643,9 +644,9 @@ def sb_count_step(tokens: torch.Tensor, result: torch.Tensor, counts: torch.Tens
     _need(tokens, 4, "tokens", torch.int32)
     _need(result, STEP_RESULT_INTS * 4, "result", torch.int32)
     _need(counts, 4, "counts", torch.int32)
-    _on_stream_device(stream, tokens, result, counts)
+    handle = _stream_on(stream, tokens, result, counts)
     _check(lib.sb_count_step(counts.numel(), tokens.numel(), tokens.data_ptr(), result.data_ptr(),
-                             counts.data_ptr(), _stream(stream)), "sb_count_step")
+                             counts.data_ptr(), handle), "sb_count_step")
 
 
 class LogitRules:
@@ -700,10 +701,10 @@ def sb_shape_logits(rules: LogitRules, tokens: torch.Tensor, parents, logits: to
     _need(stats, n * 16, "stats")
     _need(ws, 0, "ws")
     rules._check(v, n)
-    _on_stream_device(stream, tokens, logits, out, stats, ws, *rules.tensors)
+    handle = _stream_on(stream, tokens, logits, out, stats, ws, *rules.tensors)
     _check(lib.sb_shape_logits(v, n, C.byref(rules.struct), tokens.data_ptr(), pp,
                                logits.data_ptr(), out.data_ptr(), temperature, stats.data_ptr(),
-                               ws.data_ptr(), ws.nbytes, _stream(stream)), "sb_shape_logits")
+                               ws.data_ptr(), ws.nbytes, handle), "sb_shape_logits")
 
 
 def sb_sample_workspace_bytes(vocab: int) -> int:
