@@ -534,7 +534,8 @@ class QuantizedKV:
     def _of(self, cfg: ModelConfig, stream, *tensors):
         """This cache's struct for a call with cfg, once its sizes agree."""
         c = self.cfg
-        if (cfg.n_layers, cfg.n_kv_heads, cfg.head_dim) != (c.n_layers, c.n_kv_heads, c.head_dim):
+        if cfg is not c and ((cfg.n_layers, cfg.n_kv_heads, cfg.head_dim)
+                             != (c.n_layers, c.n_kv_heads, c.head_dim)):
             raise ValueError("the cache was made for another n_layers, n_kv_heads or head_dim")
         _stream_on(stream, self.k, *tensors)
         return C.byref(self._struct)
