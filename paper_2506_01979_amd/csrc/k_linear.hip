@@ -11,10 +11,10 @@
 // - k_linear, few rows: both operands straight to registers; a workgroup owns NT
 //   weight tiles and TT token tiles, its waves split K, so every wave streams its
 //   own stretch of the tiles with nothing shared until the end, where the waves'
-//   sums meet in LDS.  22016 x 4096, 33 rows: 23.4 us, 3.9 TB/s.
+//   sums meet in LDS.  22016 x 4096, 33 rows: 19 us, 4.8 TB/s.
 // - k_linear_ring, many rows: 128 or 256 channels and all rows per workgroup, so
 //   that activations are read once per that many channels; both operands through
-//   a ring of LDS stages.  57344 x 8192, 129 rows: 114 us, 4.3 TB/s (k_linear: 172).
+//   a ring of LDS stages.  57344 x 8192, 129 rows: 117 us, 4.2 TB/s (k_linear: 172).
 #include <math.h>
 
 #include "sb_internal_fwd.h"
@@ -191,8 +191,7 @@ __global__ __launch_bounds__(64 * NW) void k_linear(LinearArgs a) {
   auto load = [&](Buf &b, int s) {
 #pragma unroll
     for (int u = 0; u < kU; ++u) {
-      // past the wave's stretch: an offset past both buffers (2 MB and 4 MB at
-      // most), which reads zeros
+      // past the wave's stretch: an offset past both buffers (4 MB at most), which reads zeros
       const int vo = s + u < s1 ? (s + u) * 1024 + lane * 16 : 0x7fff0000;
 #pragma unroll
       for (int i = 0; i < NT; ++i)
@@ -358,12 +357,21 @@ hipError_t launch_form(const LinearArgs &a, hipStream_t s) {
   return hipGetLastError();
 }
 
+// Most weight tiles of a workgroup of k_linear: what the accumulators leave
+// registers for.
+constexpr int most_tiles(int tt) { return tt <= 2 ? 8 : tt == 3 ? 6 : tt == 4 ? 5 : 4; }
+
 template <int TT>
 hipError_t launch_tt(const LinearArgs &a, int nt, hipStream_t s) {
+  constexpr int NW = TT <= 4 ? 8 : 4, M = most_tiles(TT);
   switch (nt) {
-    case 1: return launch_form<1, TT, 8>(a, s);
-    case 2: return launch_form<2, TT, TT <= 4 ? 8 : 4>(a, s);
-    case 4: return launch_form<4, TT, TT <= 4 ? 8 : 4>(a, s);
+    case 1: return launch_form<1, TT, NW>(a, s);
+    case 2: return launch_form<2, TT, NW>(a, s);
+    case 3: return launch_form<3, TT, NW>(a, s);
+    case 4: return launch_form<4, TT, NW>(a, s);
+    case 5: return launch_form<M < 5 ? 4 : 5, TT, NW>(a, s);
+    case 6: return launch_form<M < 6 ? 4 : 6, TT, NW>(a, s);
+    case 8: return launch_form<M < 8 ? 4 : 8, TT, NW>(a, s);
     default: return hipErrorInvalidValue;
   }
 }
@@ -399,48 +407,57 @@ struct LinearPlan {
   int nt, tblocks, ring_tiles, splits;
 };
 
-// k_linear's workgroups read the activations once per weight tile group, the
-// ring's once per 128 or 256 channels, but the ring pays for its stages' barriers
-// and the join of K ranges, and needs a long stream.  Measured, k_linear / ring, us:
+// The kernel and its tiles by what a compute unit has to bring in, in KB (1 KB per
+// tile and k-step), as its fill rate bounds both kernels; a round of workgroups
+// costs 100 KB more.  For k_linear that is rounds (nt + tt) ks, which is least
+// where the tiles make one even round; measured, by nt, us:
+//   12288 x 4096, 33 rows    2: 18.9   3: 15.0   4: 16.3   6: 19.6
+//   22016 x 4096, 33 rows    3: 24.3   4: 27.3   5: 31.0   6: 22.5
+//   57344 x 8192, 33 rows    2: 103    4: 94.8   5: 90.8   6: 99.8
+// The ring's bytes count 1.3 times (1.43 with two tiles a wave: stages and
+// barriers), K ranges 300 KB (the join's launch) and twice their sums.  Measured,
+// k_linear / ring, us:
 //   rows                   17           33            65            129
-//   4096 x 4096         9.6 / 14.0  10.4 / 15.8   13.0 / 18.1   14.4 / -
-//   5120 x 5120        15.1 / 15.5  17.7 / 17.3   23.0 / 18.2
-//   22016 x 4096       24.1 / 24.7  26.9 / 26.6   32.6 / 28.7   43.7 / 34.4
-//   8192 x 8192        18.1 / 21.4  21.0 / 23.1   25.4 / 24.2
-//   8192 x 28672       51.6 / 53.9  60.9 / 56.7   76.5 / 61.7  100.3 / 75.1
-//   57344 x 8192       83.9 / 96.6  93.6 / 98.9  114.8 / 102.4 176.7 / 121.4
-//   10240 x 8192       26.9 / 24.9  31.9 / 26.0   39.2 / 27.9   50.0 / 34.7
-//   5120 x 13824       31.3 / 23.1  38.1 / 24.5   49.8 / 26.4   58.0 / 32.0
-// so the ring takes four or more token tiles of 24 MB of codes or more, and from
-// two on where k_linear leaves compute units idle in its last round of a long K
-// (the last two lines; on few rows k_linear is within a few percent of the stream).
+//   4096 x 4096         9.3 / 14.0  10.4 / 16.0   12.2 / 18.1   14.0 / 22.7
+//   12288 x 4096       13.6 / 17.1  15.1 / 18.6   18.0 / 20.3   26.4 / 26.1
+//   22016 x 4096       20.3 / 24.6  22.6 / 26.2   28.1 / 28.4   44.1 / 34.4
+//   5120 x 13824       26.4 / 22.9  29.9 / 24.3   36.6 / 26.5   43.6 / 32.3
+//   8192 x 28672       51.3 / 53.6  61.1 / 57.0   76.3 / 61.4  100   / 75
+//   57344 x 8192       82.2 / 95.2  90.4 / 99.3  115   / 104   178   / 118
+// One token tile is always k_linear's.
 LinearPlan linear_plan(int tiles, int ks, int n_tok) {
   LinearPlan p{};
   const int ttiles = ceil_div(n_tok, 16);
   p.splits = 1;
   p.tblocks = ceil_div(ttiles, kLinearMaxTokenTiles);
-  // tiles per workgroup: as many (up to four) as leave a workgroup for every
-  // compute unit
-  p.nt = 4;
-  while (p.nt > 1 && ceil_div(tiles, p.nt) * p.tblocks < kAttnCUs) p.nt /= 2;
-  const int groups = ceil_div(tiles, p.nt), rounds = ceil_div(groups, kAttnCUs);
-  const int64_t bytes = (int64_t)tiles * ks * 1024;
-  const bool idle = ks >= 128 && bytes >= (64 << 20) && 4 * rounds * kAttnCUs > 5 * groups;
-  if (!(ttiles >= 4 && bytes >= (24 << 20)) && !(ttiles >= 2 && ttiles <= 3 && idle)) return p;
-  // 128 channels per workgroup; 256 where that leaves as few rounds of workgroups
-  // (57344 x 8192, 224 workgroups instead of 448), or for the most rows of a long K
-  // whose ranges still fill the compute units (256 rows: 8192 x 28672 110 -> 99 us,
-  // 10240 x 8192 56 -> 54; but 4096 x 11008 38 -> 42, 128 workgroups), as then the
-  // activations are read half as often
-  const int g1 = ceil_div(tiles, kRingWaves), g2 = ceil_div(tiles, 2 * kRingWaves);
-  const bool wide = g1 > kAttnCUs ? 2 * ceil_div(g2, kAttnCUs) <= ceil_div(g1, kAttnCUs)
-                                  : ttiles > 12 && ks >= 128 && g2 * kRingMaxSplits >= kAttnCUs;
-  p.ring_tiles = ttiles >= 4 && wide ? 2 : 1;
-  // K ranges of eight k-steps or more, up to a workgroup for every compute unit
-  p.splits = kAttnCUs / (p.ring_tiles == 2 ? g2 : g1);
-  if (p.splits > kRingMaxSplits) p.splits = kRingMaxSplits;
-  if (p.splits > ks / 8) p.splits = ks / 8;
-  if (p.splits < 1) p.splits = 1;
+  const int tt = ceil_div(ttiles, p.tblocks);
+  int64_t best = INT64_MAX;
+  for (const int nt : {8, 6, 5, 4, 3, 2, 1}) {
+    if (nt > most_tiles(tt)) continue;
+    const int64_t rounds = ceil_div(ceil_div(tiles, nt) * p.tblocks, kAttnCUs);
+    const int64_t cost = rounds * ((int64_t)(nt + tt) * ks + 100);
+    if (cost < best) {
+      best = cost;
+      p.nt = nt;
+    }
+  }
+  for (int r = 1; r <= 2 && ttiles >= 2; ++r) {
+    if (r == 2 && ttiles < 4) break;
+    const int groups = ceil_div(tiles, kRingWaves * r);
+    // K ranges of eight k-steps or more, up to a workgroup for every compute unit
+    int splits = kAttnCUs / groups;
+    if (splits > kRingMaxSplits) splits = kRingMaxSplits;
+    if (splits > ks / 8) splits = ks / 8;
+    if (splits < 1) splits = 1;
+    const int64_t rounds = ceil_div(groups * splits, kAttnCUs);
+    const int64_t kb = (int64_t)(kRingWaves * r + ttiles) * ceil_div(ks, splits) * (r == 2 ? 143 : 130) / 100;
+    const int64_t sums = splits > 1 ? 300 + (int64_t)splits * ttiles * tiles / 64 : 0;
+    if (rounds * (kb + 100) + sums < best) {
+      best = rounds * (kb + 100) + sums;
+      p.ring_tiles = r;
+      p.splits = splits;
+    }
+  }
   return p;
 }
 

@@ -106,6 +106,17 @@ def test_linear_large(api, m, k, rows):
         assert np.array_equal(y[:, some.cuda()].cpu().numpy(), int8.linear(x.float().numpy(), wf))
 
 
+@pytest.mark.parametrize("m,k", [(8180, 330), (11000, 260), (17601, 130), (22000, 200), (24400, 520), (30001, 66), (57000, 72)])
+@pytest.mark.parametrize("n", [1, 16, 17, 33, 50, 70, 100, 150])
+def test_linear_tiles(api, m, k, n):
+    """One to eight weight tiles a workgroup: one even round of them, or several."""
+    g = torch.Generator().manual_seed(m + k + n)
+    say("linear tiles", m, k, n)
+    w, x = torch.randn((m, k), generator=g).bfloat16(), torch.randn((n, k), generator=g)
+    got = product(api, w, x, shift=4 * (n % 2))
+    assert np.array_equal(got, int8.linear(x.numpy(), w.float().numpy(), np.float32))
+
+
 def test_linear_large_captured(api):
     """K ranges and their join in a graph, beside eager calls on a workspace of their own."""
     m, k, n = 5003, 5128, 70
