@@ -166,7 +166,8 @@ __device__ __forceinline__ void store_scaled(const LinearArgs &a, int t, int r, 
 }
 
 // NT weight tiles x TT token tiles, NW waves; kU k-steps are in flight while
-// the kU before them are multiplied.
+// the kU before them are multiplied (four where registers allow: level on long K,
+// 0.3 to 1.5 us slower on K of 768 to 5120).
 constexpr int kU = 2;
 template <int NT, int TT, int NW>
 __global__ __launch_bounds__(64 * NW) void k_linear(LinearArgs a) {
