@@ -39,10 +39,12 @@ __global__ __launch_bounds__(kCountT) void k_count_tokens(int vocab, int n,
   cnt[threadIdx.x] = 0;
   __syncthreads();
   constexpr int kBatch = 8;
-  for (int i0 = threadIdx.x; i0 < n; i0 += kBatch * kCountT) {
+  // unsigned: the last batch of 2^31 - 1 tokens ends past them
+  for (unsigned i0 = threadIdx.x; i0 < (unsigned)n; i0 += kBatch * kCountT) {
     int t[kBatch];
 #pragma unroll
-    for (int b = 0; b < kBatch; ++b) t[b] = i0 + b * kCountT < n ? tokens[i0 + b * kCountT] : -1;
+    for (int b = 0; b < kBatch; ++b)
+      t[b] = i0 + b * kCountT < (unsigned)n ? tokens[i0 + b * kCountT] : -1;
 #pragma unroll
     for (int b = 0; b < kBatch; ++b) {
       const unsigned at = (unsigned)t[b] - (unsigned)v0;

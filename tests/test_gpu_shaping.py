@@ -43,6 +43,17 @@ def test_count_tokens(api, vocab, n):
     assert (counts[vocab:] == 77).all()
 
 
+def test_count_most_tokens(api):
+    """2^31 - 1 tokens, none in the vocabulary but some of the last."""
+    n = 2 ** 31 - 1
+    t = torch.full((n,), -1, dtype=torch.int32, device="cuda")
+    t[-5000:-1] = 3
+    counts = torch.ones(5, dtype=torch.int32, device="cuda")
+    say("count most")
+    api.sb_count_tokens(t, counts)
+    assert counts.tolist() == [1, 1, 1, 5000, 1]
+
+
 def test_count_step(api):
     V, toks = 50, [3, 4, 5, 4, 60, 6]
     for path, nxt, want in (([0, 1, 3], 7, [4, 4, 7]), ([0], 3, [3]), ([0, 4, 5], 4, [6, 4]),
