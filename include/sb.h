@@ -600,6 +600,9 @@ sb_status sb_spec_round(sb_model *target, const sb_kv_cache *t_kv, int32_t t_len
 
 /* ---- projections in 8-bit integers -------------------------------------- */
 
+/* Workspaces of the calls from here on are 16-byte aligned
+ * (SB_ERR_INVALID_ARG). */
+
 /* Most inputs of a projection. */
 #define SB_LINEAR_MAX_K 32768
 

@@ -1695,7 +1695,8 @@ sb_status sb_attend_quantized(const sb_model_config *cfg, const sb_quantized_kv 
                               int32_t n_blocks, int32_t tail_len, const void *d_q,
                               const int32_t *h_parents, int32_t n_rows, void *d_out, void *d_ws,
                               size_t ws_bytes, hipStream_t stream) {
-  if (!kv || !d_q || !d_out || !d_ws || (((uintptr_t)d_q | (uintptr_t)d_out) & 15) != 0)
+  if (!kv || !d_q || !d_out || !d_ws ||
+      (((uintptr_t)d_q | (uintptr_t)d_out | (uintptr_t)d_ws) & 15) != 0)
     return SB_ERR_INVALID_ARG;
   sb_status st = check_attention_config(cfg);
   if (st != SB_OK) return st;
@@ -1733,7 +1734,8 @@ sb_status sb_verify_forward_quantized(sb_model *m, const sb_quantized_kv *kv, in
                                       const int32_t *h_parents, int32_t n_rows, float temperature,
                                       float *d_logits, sb_row_stats *d_stats, void *d_ws,
                                       size_t ws_bytes, hipStream_t stream) {
-  if (!m || !kv || !d_tokens || !d_logits || !d_stats || !d_ws || !temperature_ok(temperature))
+  if (!m || !kv || !d_tokens || !d_logits || !d_stats || !d_ws || ((uintptr_t)d_ws & 15) != 0 ||
+      !temperature_ok(temperature))
     return SB_ERR_INVALID_ARG;
   sb_status st = check_attention_config(&m->cfg);
   if (st != SB_OK) return st;
@@ -1783,7 +1785,7 @@ sb_status sb_shape_logits(int32_t vocab, int32_t n_rows, const sb_logit_rules *r
                           float *d_out, float temperature, sb_row_stats *d_stats, void *d_ws,
                           size_t ws_bytes, hipStream_t stream) {
   if (vocab < 1 || vocab > SB_BRANCH_MAX_VOCAB || !rules || !d_tokens || !d_logits || !d_out ||
-      !d_stats || !d_ws || !temperature_ok(temperature))
+      !d_stats || !d_ws || ((uintptr_t)d_ws & 15) != 0 || !temperature_ok(temperature))
     return SB_ERR_INVALID_ARG;
   const sb_logit_rules &r = *rules;
   if (!(r.repetition > 0.0f) || !isfinite(r.repetition) || !isfinite(r.presence) ||

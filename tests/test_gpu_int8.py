@@ -249,6 +249,29 @@ def test_forward(api, sname, P, parents):
     assert np.array_equal(api.decode_stats(stats)["argmax"], logits.cpu().numpy().argmax(-1))
 
 
+def test_forward_with_k_ranges(api):
+    """A long FFN on a narrow hidden size: the down projection takes K ranges, whose sums stand
+    in the step's workspace (full of other bytes here), and is followed by the norm."""
+    shape = synth.Shape("wide_ffn", 1, 1024, 8, 8, 128, 13824, 1000, "bf16")
+    n, P, parents = 33, 20, synth.branch_parents(4, 8)
+    assert api.sb_linear_workspace_bytes(1024, 13824, n) > 2 ** 20 + 48 * 13824
+    g = np.random.default_rng(41)
+    W = gains(weights(shape), g)
+    m = api.Model(shape, api.dict_tensors(W), projections="int8")
+    K = bf16(g.standard_normal((1, 8, P, 128))).float().numpy()
+    V = bf16(g.standard_normal(K.shape)).float().numpy()
+    tokens = g.integers(0, shape.vocab, n).astype(np.int32)
+    k, v = m.new_kv(P + n)
+    m.load_kv(k, v, K, V, P)
+    logits, stats = torch.empty((n, shape.vocab), device="cuda"), api.new_stats(n)
+    ws = m.workspace(256, P)
+    ws.view(torch.uint8).fill_(0xff)
+    m.sb_verify_forward(k, v, P, torch.from_numpy(tokens).cuda(), parents, 1.0, logits, stats, ws)
+    torch.cuda.synchronize()
+    ref = int8.tree_forward(shape, W, K, V, P, tokens, parents)[0]
+    check_logits(logits.cpu().numpy(), ref, decoder.tree_forward(shape, W, K, V, P, tokens, parents, "bf16")[0])
+
+
 def test_forward_noalloc_and_timed(api):
     shape = synth.SHAPES["small_h128_bf16"]
     m = api.Model(shape, api.synth_tensors(shape), projections="int8")

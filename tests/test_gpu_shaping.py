@@ -161,6 +161,25 @@ def test_each_rule(api, rep, pres, freq, bias, mask, place, shift):
     check(got, st, shaping.shape(x["logits"], x["tokens"], parents, **r), 1.0)
 
 
+@pytest.mark.parametrize("rep", [1.2, 0.75, 1 + 2 ** -23, 2 - 2 ** -22, 3e-7, 5e6, 1e-30, 1e30])
+@pytest.mark.parametrize("tree", ["root", "chain256"])
+def test_quotients(api, rep, tree):
+    """Every size of a logit, zeros and subnormals among them, by repetitions near one and far
+    from it: the quotients and products are the rounded ones."""
+    parents, V = TREES[tree], 5004 if tree == "root" else 1001
+    g = np.random.default_rng(21)
+    x, r = case(g, V, parents, rep, 0.0, 0.0, False, "none", 4000)
+    n = len(parents)
+    x["logits"] = (g.standard_normal((n, V)) * np.exp(g.uniform(-6 if n > 1 else -100, 6 if n > 1 else 85, (n, V)))).astype(np.float32)
+    x["logits"][0, ::7] = 0.0
+    x["logits"][0, 1::7] = (g.standard_normal(len(x["logits"][0, 1::7])) * 1e-40).astype(np.float32)
+    say("quotients", rep, tree)
+    got, _ = run(api, x, r, parents, 1.0)
+    with np.errstate(over="ignore"):
+        ref = shaping.shape(x["logits"], x["tokens"], parents, **r)
+    assert np.array_equal(got, ref)
+
+
 @pytest.mark.parametrize("T", [0.0, 1.0])
 def test_values_in_masked_places_and_empty_rows(api, T):
     parents, V = [-1, 0, 1, 1, 0], 1000
@@ -266,3 +285,47 @@ def test_step_under_rules(api):
         said += [int(toks[j]) for j in r["path"][1:]] + [r["next_token"]]
         assert np.array_equal(output.cpu().numpy(), shaping.count(said, V))
         root, kv_len = r["next_token"], int(new_len.item())
+
+
+def test_serving_steps(api):
+    """A request on 8-bit weights and cache: forward, rules, walk, rollback of the tail,
+    counts and commit, step after step.  The shaped rows are the oracle's of the GPU's logits, the
+    walk its walk on them, the counts those of what was said, and lengths follow."""
+    shape = synth.SHAPES["small_gqa_bf16"]
+    m = api.Model(shape, api.synth_tensors(shape), projections="int8")
+    parents = synth.fork_parents(9, 2, 4)
+    n, V = len(parents), shape.vocab
+    g = np.random.default_rng(31)
+    cache = api.QuantizedKV(m.cfg, 192, 64 + n, "int8")
+    output, prompt = torch.zeros(V, dtype=torch.int32, device="cuda"), dev(shaping.count(g.integers(0, V, 50), V))
+    rules = api.LogitRules(prompt=prompt, output=output, repetition=1.1, presence=0.1)
+    logits, stats, res = torch.empty((n, V), device="cuda"), api.new_stats(n), api.new_result()
+    ws, sws = m.quantized_workspace(n, 3, 63), torch.empty(api.sb_sample_workspace_bytes(V), dtype=torch.uint8, device="cuda")
+    rws = torch.empty(api.sb_shape_workspace_bytes(V, n), dtype=torch.uint8, device="cuda")
+    new_len, nb, tail, said, root = torch.zeros(1, dtype=torch.int32, device="cuda"), 0, 0, [], 5
+    for step in range(24):
+        toks = np.concatenate([[root], g.integers(0, V, n - 1)]).astype(np.int32)
+        m.sb_verify_forward_quantized(cache, nb, tail, dev(toks), parents, 1.0, logits, stats, ws)
+        raw = logits.cpu().numpy()
+        api.sb_shape_logits(rules, dev(toks), parents, logits, logits, 1.0, stats, rws)
+        q = torch.softmax(logits, -1)[np.maximum(parents, 0)].contiguous()
+        u = (g.random(n) * (0.4 if step % 3 else 1.0)).astype(np.float32)
+        api.sb_accept_resample(dev(toks), parents, logits, stats, 1.0, q, dev(u), res, sws)
+        m.sb_kv_rollback(cache.tail_k, cache.tail_v, tail, res, new_len)
+        api.sb_count_step(dev(toks), res, output)
+        torch.cuda.synchronize()
+        ref = shaping.shape(raw, toks, parents, prompt=prompt.cpu().numpy(), output=shaping.count(said, V),
+                            repetition=1.1, presence=0.1)
+        assert np.array_equal(logits.cpu().numpy(), ref)
+        r = api.decode_result(res)
+        o = sampling.accept_resample(toks, parents, ref, 1.0, q.cpu().numpy(), u)
+        assert r["path"] == list(o.path) and r["next_token"] == o.next_token and r["flags"] == 0
+        said += [int(toks[j]) for j in r["path"][1:]] + [r["next_token"]]
+        assert np.array_equal(output.cpu().numpy(), shaping.count(said, V))
+        root = r["next_token"]
+        nb, tail = api.sb_kv_commit(m.cfg, cache, nb, int(new_len.item()))
+        assert 64 * nb + tail == len(said) and tail < 64
+        say("serving step", step, nb, tail)
+        if nb == 2:
+            break
+    assert nb >= 1

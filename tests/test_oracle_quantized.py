@@ -155,6 +155,7 @@ def test_attend_refusals(api):
         return api.lib.sb_attend_quantized(config(api) if cfg is None else cfg, C.byref(cache(api) if c is None else c),
                                            layer, nb, tail, q, p, n, out, ws, size, None)
     assert call(q=None) == 1 and call(out=None) == 1 and call(ws=None) == 1 and call(q=24) == 1
+    assert call(ws=24) == 1
     assert call(layer=2) == 1 and call(layer=-1) == 1 and call(nb=-1) == 1 and call(tail=-1) == 1
     assert call(n=0) == 1 and call(n=257) == 1
     assert call(p=(C.c_int32 * 3)(-1, 0, 2)) == 2

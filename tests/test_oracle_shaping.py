@@ -69,6 +69,7 @@ def test_shape_refusals(api):
     assert call(vocab=0) == 1 and call(vocab=(1 << 20) + 1) == 1 and call(n=0) == 1 and call(n=257) == 1
     for k in ("toks", "logits", "out", "stats", "ws", "p"):
         assert call(**{k: None}) == 1
+    assert call(ws=24) == 1
     assert call(p=(C.c_int32 * 3)(-1, 0, 2)) == 2
     assert call(T=-1.0) == 1 and call(T=float("inf")) == 1
     nan, inf = float("nan"), float("inf")
