@@ -261,8 +261,9 @@ __global__ __launch_bounds__(64 * kRingWaves) void k_linear_ring(LinearArgs a) {
   constexpr int WT = kRingWaves * NT;      // weight tiles of a workgroup
   constexpr int F = (WT + TT) * KS;        // fragments of a stage
   constexpr int LPW = (F + kRingWaves - 1) / kRingWaves;  // of them per wave
-  __shared__ __attribute__((aligned(16))) char r0[LPW * kRingWaves * 1024],
-      r1[LPW * kRingWaves * 1024], r2[LPW * kRingWaves * 1024];
+  // the waves without a fragment in the last turn load zeros into one more
+  constexpr int kBytes = (F + (F % kRingWaves != 0)) * 1024;
+  __shared__ __attribute__((aligned(16))) char r0[kBytes], r1[kBytes], r2[kBytes];
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int split = blockIdx.x % a.splits, tile0 = blockIdx.x / a.splits * WT;
   const int tile_bytes = a.ks * 1024;
@@ -282,7 +283,7 @@ __global__ __launch_bounds__(64 * kRingWaves) void k_linear_ring(LinearArgs a) {
       const bool in = f < F && k < s1 && (is_w ? t < wn : t - WT < a.ttiles);
       const int at = ((is_w ? t : t - WT) * a.ks + k) * 1024 + lane * 16;
       // (offsets: at most 16 tiles of 512 KB)
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(is_w ? wrs : xrs, (lds_void *)(dst + f * 1024), 16,
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(is_w ? wrs : xrs, (lds_void *)(dst + min(f, F) * 1024), 16,
                                                in ? at : 0x7fff0000, 0, 0, 0);
     }
   };
@@ -379,7 +380,10 @@ hipError_t launch_tt(const LinearArgs &a, int nt, hipStream_t s) {
 
 template <int NT, int TT>
 hipError_t launch_ring(const LinearArgs &a, hipStream_t s) {
-  constexpr int KS = 48 / (kRingWaves * NT + TT);  // three stages of at most 48 KB
+  // Three stages of 20 to 35 KB.  Half as much again is the same at two or three token
+  // tiles and slower from five on (27648 x 5120: 97 rows 40.4 -> 43.7 us, 193 rows
+  // 54.5 -> 69), a quarter less slower at seven and nine (40.4 -> 44.4).
+  constexpr int KS = 34 / (kRingWaves * NT + TT);
   const int groups = ceil_div(a.tiles, kRingWaves * NT);
   hipLaunchKernelGGL((k_linear_ring<NT, TT, KS>), dim3(groups * a.splits), dim3(64 * kRingWaves), 0,
                      s, a);
@@ -421,7 +425,7 @@ struct LinearPlan {
 //   rows                   17           33            65            129
 //   4096 x 4096         9.3 / 14.0  10.4 / 16.0   12.2 / 18.1   14.0 / 22.7
 //   12288 x 4096       13.6 / 17.1  15.1 / 18.6   18.0 / 20.3   26.4 / 26.1
-//   22016 x 4096       20.3 / 24.6  22.6 / 26.2   28.1 / 28.4   44.1 / 34.4
+//   22016 x 4096       20.3 / 24.6  22.6 / 26.2   28.1 / 28.4   44.1 / 34.2
 //   5120 x 13824       26.4 / 22.9  29.9 / 24.3   36.6 / 26.5   43.6 / 32.3
 //   8192 x 28672       51.3 / 53.6  61.1 / 57.0   76.3 / 61.4  100   / 75
 //   57344 x 8192       82.2 / 95.2  90.4 / 99.3  115   / 104   178   / 118
