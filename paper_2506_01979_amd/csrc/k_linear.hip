@@ -13,8 +13,9 @@
 //   own stretch of the tiles with nothing shared until the end, where the waves'
 //   sums meet in LDS.  22016 x 4096, 33 rows: 19 us, 4.8 TB/s.
 // - k_linear_ring, many rows: 128 or 256 channels and all rows per workgroup, so
-//   that activations are read once per that many channels; both operands through
-//   a ring of LDS stages.  57344 x 8192, 129 rows: 117 us, 4.2 TB/s (k_linear: 172).
+//   that activations are read once per that many channels, through a ring of LDS
+//   stages that its waves share; the weights, each wave's own, straight to
+//   registers.  57344 x 8192, 129 rows: 96 us, 5.2 TB/s (k_linear: 172).
 #include <math.h>
 
 #include "sb_internal_fwd.h"
@@ -248,18 +249,21 @@ __global__ __launch_bounds__(64 * NW) void k_linear(LinearArgs a) {
 }
 
 // More token tiles: a wave owns NT weight tiles and all TT token tiles, the
-// kRingWaves waves of a workgroup kRingWaves NT weight tiles, and every fragment of
-// a stage -- KS k-steps of the workgroup's weights and activations -- is read once
-// per workgroup, by direct-to-LDS loads into a ring of three stages (two in flight
-// while one is multiplied).  grid: tile groups x K ranges; K range `split` of
-// several leaves its sums, 32-bit integers, in part[split][n_tok][16 tiles].
+// kRingWaves waves of a workgroup kRingWaves NT weight tiles.  The activations of a
+// stage, KS k-steps, are read once per workgroup, by direct-to-LDS loads into a ring
+// of three stages (two in flight while one is multiplied), the weights beside them
+// into as many sets of registers.  Their non-temporal hint is worth 118 -> 100 us
+// (57344 x 8192, 129 rows, weights from HBM); weights through the ring as well, which
+// then holds half as many k-steps, measured 118 too.  grid: tile groups x K ranges;
+// K range `split` of several leaves its sums, 32-bit integers, in
+// part[split][n_tok][16 tiles].
 constexpr int kRingWaves = 8, kRingMaxSplits = 8;
 typedef __attribute__((address_space(3))) void lds_void;
 
 template <int NT, int TT, int KS>
 __global__ __launch_bounds__(64 * kRingWaves) void k_linear_ring(LinearArgs a) {
-  constexpr int WT = kRingWaves * NT;      // weight tiles of a workgroup
-  constexpr int F = (WT + TT) * KS;        // fragments of a stage
+  constexpr int WT = kRingWaves * NT;  // weight tiles of a workgroup
+  constexpr int F = TT * KS;           // activation fragments of a stage
   constexpr int LPW = (F + kRingWaves - 1) / kRingWaves;  // of them per wave
   // the waves without a fragment in the last turn load zeros into one more
   constexpr int kBytes = (F + (F % kRingWaves != 0)) * 1024;
@@ -267,58 +271,65 @@ __global__ __launch_bounds__(64 * kRingWaves) void k_linear_ring(LinearArgs a) {
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int split = blockIdx.x % a.splits, tile0 = blockIdx.x / a.splits * WT;
   const int tile_bytes = a.ks * 1024;
-  const int wn = min(WT, a.tiles - tile0);
-  const __amdgpu_buffer_rsrc_t wrs = uniform_rsrc(a.w + (size_t)tile0 * tile_bytes, wn * tile_bytes);
+  const int wt0 = tile0 + w * NT;  // the wave's own tiles; those past the last read zeros
+  const int wn = min(NT, a.tiles - wt0);
+  const __amdgpu_buffer_rsrc_t wrs =
+      uniform_rsrc(a.w + (size_t)min(wt0, a.tiles - 1) * tile_bytes, max(wn, 0) * tile_bytes);
   const __amdgpu_buffer_rsrc_t xrs = uniform_rsrc(a.x, a.ttiles * tile_bytes);
   const int s0 = (int)((int64_t)a.ks * split / a.splits), s1 = (int)((int64_t)a.ks * (split + 1) / a.splits);
-  // Stage at k-step s into a buffer: fragment f is k-step f / (WT + TT), weight
-  // tile or token tile f % (WT + TT).  Steps past s1 and tiles past the last read
-  // zeros.
-  auto issue = [&](int s, char *dst) {
+  constexpr int kPast = 0x7fff0000;  // past both buffers: reads zeros
+  struct Weights {
+    i32x4 f[KS][NT];
+  };
+  // Stage at k-step s: activation fragment f, k-step f / TT of token tile f % TT, to
+  // LDS, and the wave's own weights.  Steps past s1 and tiles past the last read
+  // zeros (offsets: at most 16 tiles of 512 KB).
+  auto issue = [&](int s, char *dst, Weights &b) {
 #pragma unroll
     for (int j = 0; j < LPW; ++j) {
       const int f = w + j * kRingWaves;  // uniform
-      const int k = s + f / (WT + TT), t = f % (WT + TT);
-      const bool is_w = t < WT;
-      const bool in = f < F && k < s1 && (is_w ? t < wn : t - WT < a.ttiles);
-      const int at = ((is_w ? t : t - WT) * a.ks + k) * 1024 + lane * 16;
-      // (offsets: at most 16 tiles of 512 KB)
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(is_w ? wrs : xrs, (lds_void *)(dst + min(f, F) * 1024), 16,
-                                               in ? at : 0x7fff0000, 0, 0, 0);
+      const int k = s + f / TT, t = f % TT;
+      const bool in = f < F && k < s1 && t < a.ttiles;
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(xrs, (lds_void *)(dst + min(f, F) * 1024), 16,
+                                               in ? (t * a.ks + k) * 1024 + lane * 16 : kPast, 0, 0, 0);
     }
+#pragma unroll
+    for (int k = 0; k < KS; ++k)
+#pragma unroll
+      for (int i = 0; i < NT; ++i)
+        b.f[k][i] = __builtin_amdgcn_raw_buffer_load_b128(
+            wrs, s + k < s1 && i < wn ? (i * a.ks + s + k) * 1024 + lane * 16 : kPast, 0, kNonTemporal);
   };
   i32x4 acc[NT][TT];
 #pragma unroll
   for (int i = 0; i < NT; ++i)
 #pragma unroll
     for (int j = 0; j < TT; ++j) acc[i][j] = i32x4{0, 0, 0, 0};
-  issue(s0, r0);
-  issue(s0 + KS, r1);
+  Weights b0, b1, b2;
+  issue(s0, r0, b0);
+  issue(s0 + KS, r1, b1);
   // The stage at s is there once every wave has waited for its own loads of it
   // (one later stage may be in flight) and met the others; then the buffer of the
   // stage before is free.
-  auto round = [&](int s, const char *cur, char *nxt) {
-    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(LPW) : "memory");
-    issue(s + 2 * KS, nxt);
+  auto round = [&](int s, const char *cur, const Weights &b, char *nxt, Weights &nb) {
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(LPW + KS * NT) : "memory");
+    issue(s + 2 * KS, nxt, nb);
+    __builtin_amdgcn_sched_barrier(0);
     if (s >= s1) return;
     const char *frag = cur + lane * 16;
 #pragma unroll
-    for (int k = 0; k < KS; ++k) {
-      i32x4 wf[NT];
-#pragma unroll
-      for (int i = 0; i < NT; ++i) wf[i] = *(const i32x4 *)(frag + (k * (WT + TT) + w * NT + i) * 1024);
+    for (int k = 0; k < KS; ++k)
 #pragma unroll
       for (int j = 0; j < TT; ++j) {
-        const i32x4 xf = *(const i32x4 *)(frag + (k * (WT + TT) + WT + j) * 1024);
+        const i32x4 xf = *(const i32x4 *)(frag + (k * TT + j) * 1024);
 #pragma unroll
-        for (int i = 0; i < NT; ++i) acc[i][j] = mfma16i(wf[i], xf, acc[i][j]);
+        for (int i = 0; i < NT; ++i) acc[i][j] = mfma16i(b.f[k][i], xf, acc[i][j]);
       }
-    }
   };
   for (int s = s0; s < s1; s += 3 * KS) {
-    round(s, r0, r2);
-    round(s + KS, r1, r0);
-    round(s + 2 * KS, r2, r1);
+    round(s, r0, b0, r2, b2);
+    round(s + KS, r1, b1, r0, b0);
+    round(s + 2 * KS, r2, b2, r1, b1);
   }
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // loads into LDS still in flight
   // element e of lane l is channel 4 (l / 16) + e of the tile, token l % 16
@@ -380,10 +391,10 @@ hipError_t launch_tt(const LinearArgs &a, int nt, hipStream_t s) {
 
 template <int NT, int TT>
 hipError_t launch_ring(const LinearArgs &a, hipStream_t s) {
-  // Three stages of 20 to 35 KB.  Half as much again is the same at two or three token
-  // tiles and slower from five on (27648 x 5120: 97 rows 40.4 -> 43.7 us, 193 rows
-  // 54.5 -> 69), a quarter less slower at seven and nine (40.4 -> 44.4).
-  constexpr int KS = 34 / (kRingWaves * NT + TT);
+  // Twice as long stages: 57344 x 8192, 65 rows 84.5 -> 91.7 us, 129 rows 98 -> 103,
+  // 5120 x 13824, 33 rows 24.6 -> 27.2.  (Two weight tiles and twelve or more token
+  // tiles: 1 for 2, 256 rows 140 -> 150.)
+  constexpr int KS = TT <= 3 ? 4 : TT <= 9 || NT == 2 ? 2 : 1;
   const int groups = ceil_div(a.tiles, kRingWaves * NT);
   hipLaunchKernelGGL((k_linear_ring<NT, TT, KS>), dim3(groups * a.splits), dim3(64 * kRingWaves), 0,
                      s, a);
@@ -424,11 +435,11 @@ struct LinearPlan {
 // k_linear / ring, us:
 //   rows                   17           33            65            129
 //   4096 x 4096         9.3 / 14.0  10.4 / 16.0   12.2 / 18.1   14.0 / 22.7
-//   12288 x 4096       13.6 / 17.1  15.1 / 18.6   18.0 / 20.3   26.4 / 26.1
-//   22016 x 4096       20.3 / 24.6  22.6 / 26.2   28.1 / 28.4   44.1 / 34.2
-//   5120 x 13824       26.4 / 22.9  29.9 / 24.3   36.6 / 26.5   43.6 / 32.3
-//   8192 x 28672       51.3 / 53.6  61.1 / 57.0   76.3 / 61.4  100   / 75
-//   57344 x 8192       82.2 / 95.2  90.4 / 99.3  115   / 104   178   / 118
+//   12288 x 4096       13.6 / 17.1  15.1 / 18.6   18.0 / 20.3   26.1 / 26.1
+//   22016 x 4096       20.3 / 24.6  22.6 / 26.2   28.1 / 28.3   44.1 / 33.9
+//   5120 x 13824       26.4 / 22.9  29.9 / 24.5   36.6 / 28.3   43.6 / 34.7
+//   8192 x 28672       51.3 / 53.6  61.1 / 52.4   76.3 / 61.0  100   / 76.8
+//   57344 x 8192       82.2 / 95.2  90.4 / 99.3  115   / 85.0  178   / 100
 // One token tile is always k_linear's.
 LinearPlan linear_plan(int tiles, int ks, int n_tok) {
   LinearPlan p{};
