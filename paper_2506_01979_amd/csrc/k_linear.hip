@@ -407,8 +407,8 @@ hipError_t launch_ring(const LinearArgs &a, hipStream_t s) {
 // there cost nothing next to the weights' bytes.
 template <int NT>
 hipError_t launch_ring_tt(const LinearArgs &a, hipStream_t s) {
-  if (NT == 1 && a.ttiles <= 2) return launch_ring<1, 2>(a, s);
-  if (NT == 1 && a.ttiles <= 3) return launch_ring<1, 3>(a, s);
+  if (a.ttiles <= 2) return launch_ring<NT, 2>(a, s);
+  if (a.ttiles <= 3) return launch_ring<NT, 3>(a, s);
   if (a.ttiles <= 5) return launch_ring<NT, 5>(a, s);
   if (a.ttiles <= 7) return launch_ring<NT, 7>(a, s);
   if (a.ttiles <= 9) return launch_ring<NT, 9>(a, s);
@@ -430,16 +430,17 @@ struct LinearPlan {
 //   12288 x 4096, 33 rows    2: 18.9   3: 15.0   4: 16.3   6: 19.6
 //   22016 x 4096, 33 rows    3: 24.3   4: 27.3   5: 31.0   6: 22.5
 //   57344 x 8192, 33 rows    2: 103    4: 94.8   5: 90.8   6: 99.8
-// The ring's bytes count 1.3 times (1.43 with two tiles a wave: stages and
-// barriers), K ranges 300 KB (the join's launch) and twice their sums.  Measured,
-// k_linear / ring, us:
+// The ring's bytes count 1.3 times (1.25 with two tiles a wave: stages and
+// barriers), K ranges 300 KB (the join's launch) and twice their sums.  (45000 x
+// 5120 with one tile a wave, or k_linear, against two: 49 rows 58.7 / 48.2, 65 rows
+// 63.2 / 50.2.)  Measured, k_linear / ring, us:
 //   rows                   17           33            65            129
 //   4096 x 4096         9.3 / 14.0  10.4 / 16.0   12.2 / 18.1   14.0 / 22.7
 //   12288 x 4096       13.6 / 17.1  15.1 / 18.6   18.0 / 20.3   26.1 / 26.1
 //   22016 x 4096       20.3 / 24.6  22.6 / 26.2   28.1 / 28.3   44.1 / 33.9
 //   5120 x 13824       26.4 / 22.9  29.9 / 24.5   36.6 / 28.3   43.6 / 34.7
 //   8192 x 28672       51.3 / 53.6  61.1 / 52.4   76.3 / 61.0  100   / 76.8
-//   57344 x 8192       82.2 / 95.2  90.4 / 99.3  115   / 85.0  178   / 100
+//   57344 x 8192       82.2 / 95.2  90.4 / 86.7  115   / 85.0  178   / 98
 // One token tile is always k_linear's.
 LinearPlan linear_plan(int tiles, int ks, int n_tok) {
   LinearPlan p{};
@@ -458,7 +459,6 @@ LinearPlan linear_plan(int tiles, int ks, int n_tok) {
     }
   }
   for (int r = 1; r <= 2 && ttiles >= 2; ++r) {
-    if (r == 2 && ttiles < 4) break;
     const int groups = ceil_div(tiles, kRingWaves * r);
     // K ranges of eight k-steps or more, up to a workgroup for every compute unit
     int splits = kAttnCUs / groups;
@@ -466,7 +466,7 @@ LinearPlan linear_plan(int tiles, int ks, int n_tok) {
     if (splits > ks / 8) splits = ks / 8;
     if (splits < 1) splits = 1;
     const int64_t rounds = ceil_div(groups * splits, kAttnCUs);
-    const int64_t kb = (int64_t)(kRingWaves * r + ttiles) * ceil_div(ks, splits) * (r == 2 ? 143 : 130) / 100;
+    const int64_t kb = (int64_t)(kRingWaves * r + ttiles) * ceil_div(ks, splits) * (r == 2 ? 125 : 130) / 100;
     const int64_t sums = splits > 1 ? 300 + (int64_t)splits * ttiles * tiles / 64 : 0;
     if (rounds * (kb + 100) + sums < best) {
       best = rounds * (kb + 100) + sums;

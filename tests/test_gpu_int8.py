@@ -117,6 +117,41 @@ def test_linear_tiles(api, m, k, n):
     assert np.array_equal(got, int8.linear(x.numpy(), w.float().numpy(), np.float32))
 
 
+@pytest.mark.parametrize("m,k", [(1030, 13800), (57500, 1030)])
+@pytest.mark.parametrize("n", [17, 33, 50, 70, 100, 140, 190, 256])
+def test_linear_shared_stages(api, m, k, n):
+    """Every number of token tiles that workgroups share, on K ranges of one product and on whole
+    ones of 256 channels a workgroup."""
+    g = torch.Generator().manual_seed(m + k + n)
+    say("linear shared", m, k, n)
+    w, x = torch.randn((m, k), generator=g).bfloat16(), torch.randn((n, k), generator=g).bfloat16()
+    got = product(api, w, x, shift=n % 4)
+    assert np.array_equal(got, int8.linear(x.float().numpy(), w.float().numpy()))
+
+
+def test_linear_k_ranges_captured(api):
+    """K ranges and their join replayed, beside eager calls on a workspace of their own."""
+    m, k, n = 1030, 13800, 70
+    assert api.sb_linear_workspace_bytes(m, k, n) > 2 ** 20 + 80 * 13824
+    g = torch.Generator().manual_seed(6)
+    packed = torch.empty(api.sb_linear_packed_bytes(m, k), dtype=torch.uint8, device="cuda")
+    api.sb_linear_pack(torch.randn((m, k), generator=g).bfloat16().cuda(), packed)
+    x0 = torch.randn((n, k), generator=g).cuda()
+    xd, y, y2 = x0.clone(), torch.zeros((n, m), device="cuda"), torch.zeros((n, m), device="cuda")
+    ws, ws2 = (torch.empty(api.sb_linear_workspace_bytes(m, k, n), dtype=torch.uint8, device="cuda") for _ in range(2))
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        api.sb_linear_quantized(packed, xd, y, ws)
+    for i in range(4):
+        xd.copy_(x0 * (3.0 if i % 2 else -1.0) + i)
+        y.zero_()
+        graph.replay()
+        api.sb_linear_quantized(packed, xd, y2, ws2)
+        torch.cuda.synchronize()
+        assert torch.equal(y, y2) and y.abs().max() > 0
+
+
 def test_linear_large_captured(api):
     """K ranges and their join in a graph, beside eager calls on a workspace of their own."""
     m, k, n = 5003, 5128, 70
