@@ -329,3 +329,27 @@ def test_serving_steps(api):
         if nb == 2:
             break
     assert nb >= 1
+
+
+def test_captured_large_tree(api):
+    """A tree of more than 128 rows, whose paths stand in the workspace, replayed beside eager calls
+    for other trees on a workspace of their own."""
+    V, parents = 1500, [-1] + [i // 2 for i in range(199)]
+    n, g = len(parents), np.random.default_rng(17)
+    x, r = case(g, V, parents, 1.2, 0.2, 0.1, False, "none")
+    rules, toks, logits = rules_on_device(api, r), dev(x["tokens"], np.int32), dev(x["logits"])
+    out, stats = torch.zeros((n, V), device="cuda"), api.new_stats(n)
+    ws, ws2 = (torch.empty(api.sb_shape_workspace_bytes(V, 256), dtype=torch.uint8, device="cuda") for _ in range(2))
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        api.sb_shape_logits(rules, toks, parents, logits, out, 1.0, stats, ws)
+    for i in range(3):
+        toks.copy_(dev(g.integers(0, V, n), np.int32) if i else toks)
+        other, st2 = torch.zeros((n, V), device="cuda"), api.new_stats(n)
+        api.sb_shape_logits(rules, toks, list(range(-1, n - 1)), logits, other, 1.0, st2, ws2)
+        graph.replay()
+        torch.cuda.synchronize()
+        t = toks.cpu().numpy()
+        check(out.cpu().numpy(), api.decode_stats(stats), shaping.shape(x["logits"], t, parents, **r), 1.0)
+        check(other.cpu().numpy(), api.decode_stats(st2), shaping.shape(x["logits"], t, list(range(-1, n - 1)), **r), 1.0)
