@@ -1,6 +1,6 @@
 """The serving operators around the verify step: plain forms, exact forms, cases.
 
-Five operators, at the sizes of the framework's own models (the 68M draft, the
+Four operators, at the sizes of the framework's own models (the 68M draft, the
 7B, 13B and 70B widths):
 
 * ``quantize``  blocks of 64 cached tokens to 8 bits with one scale per block
@@ -8,8 +8,6 @@ Five operators, at the sizes of the framework's own models (the 68M draft, the
 * ``attend``    the branch-masked attention of one layer over such a cache: the
   8-bit blocks, the 16-bit tail behind them and the tree's own rows;
 * ``count``     how often every token of the vocabulary occurs in a list;
-* ``linear``    a projection in 8-bit integers, with a scale for each token and
-  each output channel;
 * ``shape``     penalties for repeated tokens, biases and grammar masks on the
   logits of a token tree, with the softmax statistics of the result.
 
@@ -33,18 +31,13 @@ MODELS = {
     "llama13b": (40, 40, 40, 128, 32000),
     "llama70b": (80, 64, 8, 128, 128256),
 }
-# [output channels][inputs] of their projections: Q, K and V; O; gate and up; down; the LM head
-LINEARS = {
-    "draft68m": [(2304, 768), (768, 768), (32000, 768)],
-    "llama7b": [(12288, 4096), (4096, 4096), (22016, 4096), (4096, 11008), (32000, 4096)],
-    "llama13b": [(15360, 5120), (5120, 5120), (27648, 5120), (5120, 13824), (32000, 5120)],
-    "llama70b": [(10240, 8192), (8192, 8192), (57344, 8192), (8192, 28672)],
-}
 FORMATS = {"int8": 127.0, "e4m3": 448.0}
 
 
 def listed():
     return [
+        # the 68M draft's cache after 64 more committed tokens: the smallest commit
+        dict(name="quantize_draft68m_1", kind="quantize", model="draft68m", layers=2, blocks=1, format="int8"),
         # a 256-row chunk of prefill on the 7B cache
         dict(name="quantize_7b_4", kind="quantize", model="llama7b", layers=32, blocks=4, format="int8"),
         # a whole 4096-token prefix of the 70B cache, taken over from 16 bits
@@ -55,12 +48,10 @@ def listed():
         dict(name="attend_7b_33rows", kind="attend", model="llama7b", blocks=31, tail=63, trunk=0, branches=4, depth=8, format="int8"),
         # the widest tree of the 13B sweep at its longest prefix
         dict(name="attend_13b_129rows", kind="attend", model="llama13b", blocks=127, tail=63, trunk=0, branches=8, depth=16, format="e4m3"),
+        # grouped queries: 264 query rows on each of 8 KV heads
+        dict(name="attend_70b_33rows", kind="attend", model="llama70b", blocks=63, tail=63, trunk=0, branches=4, depth=8, format="int8"),
         # one token over a long context: the cache's bytes and nothing else
         dict(name="attend_70b_1row_long", kind="attend", model="llama70b", blocks=512, tail=5, trunk=0, branches=0, depth=0, format="e4m3"),
-        # the benchmark's largest projection, 33 rows on the 7B gate and up
-        dict(name="linear_7b_33rows", kind="linear", outputs=22016, inputs=4096, rows=33),
-        # the widest tree on the 70B gate and up
-        dict(name="linear_70b_129rows", kind="linear", outputs=57344, inputs=8192, rows=129),
         # a short prompt's counts at the start of a request
         dict(name="count_33", kind="count", vocab=32000, n=33),
         # a long document's
@@ -92,7 +83,7 @@ def _tree(rng, most):
 
 
 def draw(rng):
-    kind = rng.choice(["quantize", "attend", "attend", "attend", "linear", "linear", "count", "shape", "shape"])
+    kind = rng.choice(["quantize", "attend", "attend", "attend", "count", "shape", "shape"])
     if kind == "quantize":
         model = rng.choice(list(MODELS))
         layers = rng.randint(1, MODELS[model][0])
@@ -107,15 +98,6 @@ def draw(rng):
                         **_tree(rng, 256), format=rng.choice(list(FORMATS)))
             w = work(case)
             if w["bytes"] <= most["bytes"] and w["flops"] <= most["flops"]:
-                return case
-    if kind == "linear":
-        most = work(next(c for c in listed() if c["name"] == "linear_70b_129rows"))
-        while True:
-            outputs, inputs = rng.choice(LINEARS[rng.choice(list(LINEARS))])
-            if rng.random() < 0.25:  # widths of no model
-                outputs, inputs = _log_int(rng, 100, outputs), 8 * _log_int(rng, 8, inputs // 8)
-            case = dict(kind=kind, outputs=outputs, inputs=inputs, rows=_log_int(rng, 1, 256))
-            if work(case)["flops"] <= most["flops"]:
                 return case
     vocab = rng.choice([32000, 32000, 128256, _log_int(rng, 1000, 128256)])
     if kind == "count":
@@ -166,13 +148,6 @@ def _attend_inputs(case, seed):
     return k[0], v[0], _normal(g, (n, nh, d), 1.5).bfloat16()
 
 
-def _linear_inputs(case, seed):
-    """A weight matrix, and activations with a few channels larger than the rest; bf16."""
-    g, m, k = _generator(seed, 5), case["outputs"], case["inputs"]
-    channel = torch.exp(_normal(g, (k,), 0.5))
-    return _normal(g, (m, k), 0.02, torch.bfloat16), (_normal(g, (case["rows"], k)) * channel).bfloat16()
-
-
 def _quantize_inputs(case, seed):
     _, _, nkv, d, _ = MODELS[case["model"]]
     return _cache(_generator(seed, 2), case["layers"], nkv, BLOCK * case["blocks"], d)
@@ -216,17 +191,6 @@ def prepare(case, seed):
     if case["kind"] == "count":
         g = _generator(seed, 4)
         return dict(s, tokens=_text(g, case["vocab"], case["n"]), counts=torch.zeros(case["vocab"], dtype=torch.int32, device=DEVICE))
-    if case["kind"] == "linear":
-        w, s["x"] = _linear_inputs(case, seed)
-        if own:
-            api, (m, k) = _api(), w.shape
-            s["w"] = torch.empty(api.sb_linear_packed_bytes(m, k), dtype=torch.uint8, device=DEVICE)
-            api.sb_linear_pack(w, s["w"])
-            s["y"] = torch.empty((case["rows"], m), device=DEVICE)
-            s["ws"] = torch.empty(api.sb_linear_workspace_bytes(m, k, case["rows"]), dtype=torch.uint8, device=DEVICE)
-        else:
-            s["w"], s["w_scale"] = _quantized(w, (1,), "int8")
-        return s
     if case["kind"] == "shape":
         s.update(_shape_inputs(case, seed), parents=_parents(case), paths=_paths(case))
         s["out"] = torch.empty_like(s["logits"])
@@ -283,12 +247,6 @@ def run(s):
             api.sb_count_tokens(s["tokens"], s["counts"], accumulate=False)
             return s["counts"]
         return _counts(s["tokens"], case["vocab"])
-    if case["kind"] == "linear":
-        if own:
-            api.sb_linear_quantized(s["w"], s["x"], s["y"], s["ws"])
-            return s["y"]
-        code, scale = _quantized(s["x"], (1,), "int8")
-        return torch.matmul(code.float(), s["w"].float().t()) * scale * s["w_scale"].t()
     if case["kind"] == "shape":
         if own:
             api.sb_shape_logits(s["rules"], s["tokens"], s["parents"], s["logits"], s["out"], case["temperature"], s["stats"], s["ws"])
@@ -360,9 +318,6 @@ def _shape_plain(s):
 def work(case):
     if case["kind"] == "count":
         return {"bytes": 4 * case["n"] + 4 * case["vocab"], "flops": case["n"]}
-    if case["kind"] == "linear":
-        m, k, n = case["outputs"], case["inputs"], case["rows"]
-        return {"bytes": m * k + 4 * m + 2 * n * k + 4 * n * m, "flops": 2 * n * m * k}
     n = 1 + case.get("trunk", 0) + case.get("branches", 0) * case.get("depth", 0)
     if case["kind"] == "shape":
         v, rows = case["vocab"], {"none": 0, "one": 1, "rows": n}[case["mask"]]
@@ -402,13 +357,6 @@ def _blocks64(x, form):
 def exact(case, seed):
     if case["kind"] == "count":
         return None
-    if case["kind"] == "linear":
-        (w, x), out = _linear_inputs(case, seed), []
-        for y in (w, x):
-            y = y.double()
-            amax = y.abs().max(-1, keepdim=True).values
-            out += [torch.round(y * 127 / amax), (amax / 127).float().double()]
-        return (out[2] @ out[0].t()) * out[3] * out[1].t()
     if case["kind"] == "quantize":
         k, v = _quantize_inputs(case, seed)
         k, ks = _blocks64(k, case["format"])
