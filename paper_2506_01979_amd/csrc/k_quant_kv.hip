@@ -4,7 +4,9 @@
 // A block is 64 tokens x head_dim of one (layer, KV head), of K or V:
 //   amax = max |x|, scale = fl32(amax / top), code = nearest(x top / amax),
 //   top = 127 (int8) or 448 (e4m3).
-// x has 8 significant bits and top at most 7, so x top is exact in float32 and
+// x has 8 significant bits and top at most 7, so x top is exact in float32 (of a
+// block with amax >= 2^100, whose x top may pass float32, x and amax are taken at
+// 2^-16: values that this rounds are below 2^-200 of amax, code 0), and
 // one IEEE division gives the code of the formula: the quotient of two such
 // numbers either is a tie of the 8-bit type exactly (and then a float32) or
 // lies at least 2^-17 of its size away from one, far outside the division's
@@ -76,6 +78,8 @@ __global__ __launch_bounds__(kT) void k_kv_quantize(QuantKvArgs a) {
   const size_t block = (size_t)head * a.cap_blocks + a.block + b;
   if (threadIdx.x == 0) (is_v ? a.v_scale : a.k_scale)[block] = finite ? amax / kTop : NAN;
   const bool codes = finite && top != 0;
+  const float down = amax >= 0x1p100f ? 0x1p-16f : 1.0f;
+  const float num = kTop * down, den = amax * down;
   uint8_t *dst = (is_v ? a.v : a.k) + block * (SB_KV_BLOCK * D);
 #pragma unroll
   for (int j = 0; j < IPT; ++j) {
@@ -87,7 +91,7 @@ __global__ __launch_bounds__(kT) void k_kv_quantize(QuantKvArgs a) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         const float v = bf2f((uint16_t)(w[e >> 1] >> (16 * (e & 1))));
-        y[e] = codes ? v * kTop / amax : 0.0f;
+        y[e] = codes ? v * num / den : 0.0f;
       }
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
