@@ -20,13 +20,15 @@ from . import decoder, tree
 
 def quantize(x: np.ndarray, dt=np.float64):
     """Codes and float32 scales of the rows of x.  dt float32: 127 x and the
-    quotient each rounded to float32, as for float32 activations."""
+    quotient each rounded to float32, as for float32 activations (to 24 bits also
+    where 127 x is past float32: rows of such values are taken at 2^-16)."""
     x = np.asarray(x, dt)
     with np.errstate(invalid="ignore", divide="ignore", over="ignore"):
         amax = np.abs(x).max(-1, keepdims=True)
         ok = np.isfinite(amax)
         scale = np.where(ok, amax.astype(np.float32) / np.float32(127), np.float32(np.nan))
-        codes = np.where(ok & (amax > 0), np.rint(x * dt(127) / amax), 0)
+        down = np.where(amax >= dt(2.0 ** 100), dt(2.0 ** -16), dt(1))
+        codes = np.where(ok & (amax > 0), np.rint(x * down * dt(127) / (amax * down)), 0)
     return codes.astype(np.float64), scale[..., 0].astype(np.float32)
 
 

@@ -14,15 +14,19 @@ __device__ __forceinline__ size_t item_offset(int row, int item, int ks) {
 }
 
 // Sixteen values to codes: nearest(127 x / amax), ties to even, one IEEE
-// division each (inv_live: amax is positive and finite; otherwise zeros).
+// division each (live: amax is positive and finite; otherwise zeros).  From amax =
+// 2^100 on, where 127 x may pass float32, x and amax are taken at 2^-16: the
+// same quotients but for values below 2^-200 of amax, code 0.
 __device__ __forceinline__ uint4 codes16(const float (&x)[16], float amax, bool live) {
+  const float down = amax >= 0x1p100f ? 0x1p-16f : 1.0f;
+  const float num = 127.0f * down, den = amax * down;
   uint32_t w[4];
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
     w[j] = 0;
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      const int q = live ? (int)rintf(x[4 * j + e] * 127.0f / amax) : 0;
+      const int q = live ? (int)rintf(x[4 * j + e] * num / den) : 0;
       w[j] |= (uint32_t)(q & 0xff) << (8 * e);
     }
   }
