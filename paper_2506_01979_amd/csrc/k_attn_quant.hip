@@ -26,10 +26,10 @@
 // multiplies the softmax weights,
 //   S^T = K Q^T;  w = exp2(s kscale c - m + log2 r);  l += w / r;  O^T += V^T w^T,
 //   r = vscale 2^15 / (the largest vscale of the wave's blocks),
-// so that w <= 2^15 is binary16 to 11 bits down to 2^-29 of the largest
-// weight.  Those 11 bits are the products' rounding point: an eighth of what
-// the output's bfloat16 keeps, and one matrix instruction where the two parts
-// of k_attn.hip take two.  Q enters as binary16 scaled by a power of two per
+// so that w <= 2^15 in two binary16 parts, a product each, keeps 22 bits, down to steps
+// of 2^-40 of the largest weight: no less than the two bfloat16 parts of k_attn.hip.
+// (One part, 11 bits, moves 9 % of the bfloat16 outputs by a step; 13B, 129 rows,
+// prefix 8192 49.6 us with it, 57.0 with two; 7B, 33 rows 14.2 and 14.4.)  Q enters as binary16 scaled by a power of two per
 // row (largest magnitude in [2^14, 2^15)): exact for elements down to 2^-28 of it.
 // l sums the unrounded float32 w.
 //
@@ -67,6 +67,22 @@ __device__ __forceinline__ f32x4 mfma16h(f16x8 a, f16x8 b, f32x4 c) {
 __device__ __forceinline__ uint32_t pack_f16x2(float lo, float hi) {
   const f32x2 v = {lo, hi};
   return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, f16x2));
+}
+
+// Eight floats in [0, 2^15] as two binary16 parts, 22 bits of each down to 2^-24.
+__device__ __forceinline__ void split_f16(const float (&x)[8], f16x8 &hi, f16x8 &lo) {
+  // a factor that the compiler does not know, so that widening, (exact) difference
+  // and rounding stay one instruction
+  float minus = -1.0f;
+  asm("" : "+s"(minus));
+#pragma unroll
+  for (int e = 0; e < 8; e += 2) {
+    const f16x2 h = __builtin_convertvector(f32x2{x[e], x[e + 1]}, f16x2);
+    hi[e] = h[0];
+    hi[e + 1] = h[1];
+    lo[e] = (_Float16)fmaf((float)h[0], minus, x[e]);
+    lo[e + 1] = (_Float16)fmaf((float)h[1], minus, x[e + 1]);
+  }
 }
 
 // Four codes to binary16, exactly.
@@ -322,7 +338,6 @@ struct Tiles {
     }
     scored();
     // element e of s[rt][2 h + i] is key 32 h + 8 lg + 4 i + e
-    f16x8 p[RT][2];
     float ck[RT], nm[RT];
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
@@ -334,34 +349,35 @@ struct Tiles {
       nm[rt] = max_x32(max_x16(mx)) * ck[rt];
     }
     raise(nm);
+    // 32 keys at a time: the weights of the second half beside the products of the first
+    float ps[RT];
 #pragma unroll
-    for (int rt = 0; rt < RT; ++rt) {
-      const float base = bs.lr2 - (m[rt] == -INFINITY ? 0.0f : m[rt]);
-      float ps = 0.0f;
+    for (int h = 0; h < 2; ++h) {
+      f16x8 hi[RT], lo[RT];
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
+      for (int rt = 0; rt < RT; ++rt) {
+        const float base = bs.lr2 - (m[rt] == -INFINITY ? 0.0f : m[rt]);
         float x[8];
+        if (h == 0) ps[rt] = 0.0f;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           x[e] = __builtin_amdgcn_exp2f(fmaf(s[rt][2 * h + (e >> 2)][e & 3], ck[rt], base));
-          ps += x[e];
+          ps[rt] += x[e];
         }
-        p[rt][h] = __builtin_bit_cast(f16x8, make_uint4(pack_f16x2(x[0], x[1]), pack_f16x2(x[2], x[3]),
-                                                        pack_f16x2(x[4], x[5]), pack_f16x2(x[6], x[7])));
+        split_f16(x, hi[rt], lo[rt]);
+        if (h == 1) l[rt] = fmaf(ps[rt], bs.ir, l[rt]);
+        if (TIGHT) __builtin_amdgcn_sched_barrier(0);
       }
-      l[rt] = fmaf(ps, bs.ir, l[rt]);
-      if (TIGHT) __builtin_amdgcn_sched_barrier(0);
-    }
 #pragma unroll
-    for (int dt = 0; dt < NF; ++dt) {
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
+      for (int dt = 0; dt < NF; ++dt) {
         const uint2 f = vfrag(dt, h);
         const f16x8 vv = widen8<FMT>(f.x, f.y);
 #pragma unroll
-        for (int rt = 0; rt < RT; ++rt) o[rt][dt] = mfma16h(vv, p[rt][h], o[rt][dt]);
+        for (int rt = 0; rt < RT; ++rt) o[rt][dt] = mfma16h(vv, hi[rt], o[rt][dt]);
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) o[rt][dt] = mfma16h(vv, lo[rt], o[rt][dt]);
+        if (TIGHT && (dt & 1)) __builtin_amdgcn_sched_barrier(0);
       }
-      if (TIGHT && (dt & 1)) __builtin_amdgcn_sched_barrier(0);
     }
   }
   // One step of 32 tail keys.  q(rt, j): bfloat16 query fragment; kfrag(i, j):

@@ -1,11 +1,12 @@
-"""GPU tests of the 8-bit cache where it can go wrong: the largest finite values."""
+"""GPU tests of the 8-bit cache where it can go wrong: the largest finite values
+and the bits of the softmax weights."""
 import numpy as np
 import pytest
 import torch
 
 from gpu_util import say
 from oracle import quantized
-from test_gpu_quantized import bf16, dev
+from test_gpu_quantized import bf16, dev, host, random_tree
 
 pytestmark = pytest.mark.gpu
 
@@ -49,3 +50,78 @@ def test_quantize_largest_values(api, form, d):
     for out, scale in ((ko, c.k_scale), (vo.transpose(2, 3), c.v_scale)):
         assert np.array_equal(scale.cpu().numpy(), s)
         assert np.array_equal(out.float().cpu().numpy(), ref)
+
+
+# ---- attention ---------------------------------------------------------------------
+
+def exact_cache(api, g, form, nh, nkv, d, nb, tail, parents, layers=1):
+    """A cache whose values the 8-bit type holds exactly (codes times powers of two),
+    queries of small whole numbers: scores and their sums are exact in float32."""
+    n, keys = len(parents), 64 * nb + tail + len(parents)
+    top = quantized.TOP[form]
+
+    def values(step):
+        x = quantized.nearest(g.uniform(-top / 2, top / 2, (nkv, keys, d)), form)
+        x[:, 5:64 * nb:64, 0] = top                        # every block's largest
+        return bf16(x * step)
+    k, v = values(2.0 ** -3), values(2.0 ** -9)
+    q = bf16(g.integers(-2, 3, (n, nh, d)) * (1.0 if form == "int8" else 0.25))
+    cfg = api.attention_config(layers, nh, nkv, d)
+    c = api.QuantizedKV(cfg, 64 * max(nb, 1), tail + n, form)
+    cut = 64 * nb
+    if nb:
+        api.sb_kv_quantize(cfg, dev(k[None, :, :cut]), dev(v[None, :, :cut].transpose(2, 3)), 0, c, 0, nb)
+        for x in (k, v):
+            codes, s = quantized.quantize(x[:, :cut].double().numpy(), form)
+            assert np.array_equal(quantized.values(codes, s), x[:, :cut].double().numpy())
+    c.tail_k[0, :, :tail + n] = dev(k[:, cut:])
+    c.tail_v[0, :, :, :tail + n] = dev(v[:, cut:].transpose(1, 2))
+    return cfg, c, k, v, q
+
+
+def attend(api, cfg, c, nb, tail, q, parents):
+    n = len(parents)
+    ws = torch.full((api.sb_attend_workspace_bytes(cfg, n, nb, tail),), 0xff, dtype=torch.uint8, device="cuda")
+    out = torch.full(q.shape, 9.0, dtype=torch.bfloat16, device="cuda")
+    api.sb_attend_quantized(cfg, c, 0, nb, tail, dev(q), parents, out, ws)
+    torch.cuda.synchronize()
+    return out
+
+
+def on_path(parents):
+    on = np.eye(len(parents), dtype=bool)
+    for i in range(1, len(parents)):
+        on[i] |= on[parents[i]]
+    return on
+
+
+@pytest.mark.parametrize("form", FORMATS)
+@pytest.mark.parametrize("nh,nkv,d,nb,tail,n", [(4, 4, 64, 3, 1, 1), (8, 2, 64, 9, 40, 17), (8, 2, 128, 1, 0, 1),
+                                                (4, 2, 128, 20, 33, 33), (2, 2, 128, 130, 5, 129), (2, 1, 64, 130, 5, 88)])
+def test_attend_keeps_the_weights(api, form, nh, nkv, d, nb, tail, n):
+    """The output is the bfloat16 nearest to a value that is within 2^-15 sum p |v| of the
+    exact one.  What the scores and weights lose on the way: K, V and q enter exactly
+    and the sums of q k are exact, as every term is a multiple of one step and they
+    stay below 2^24 of them.  A score in the softmax's units of log 2 is below 64 in
+    size; its factor is three roundings (3 2^-24), the sum with the maximum one more
+    of a number below 128 (2^-18), both times log 2: 2^-17.4 of a weight at most.  The
+    exponential, 1 / r and log r: 2^-20.  A weight in two parts of 8 or of 11 bits keeps
+    2^-18.  Sums of at most 2^14 weights in float32, in four or more parts: 2^-24 times
+    their steps, 2^-17 if they all fall one way.  Together below 2^-15.  (Weights of 11
+    bits: 2^-12 on the average of a weight.)"""
+    g = np.random.default_rng(100 * nb + n)
+    parents = random_tree(g, n)
+    say("attend, weights", form, nh, nkv, d, nb, tail, n)
+    cfg, c, k, v, q = exact_cache(api, g, form, nh, nkv, d, nb, tail, parents)
+    out = host(attend(api, cfg, c, nb, tail, q, parents))
+    ref, size = quantized.attend(q.double().numpy(), k.double().numpy(), v.double().numpy(), on_path(parents))
+    delta = 2.0 ** -15 * size
+    low, high = (nearest_bf16(ref + f * delta) for f in (-1, 1))
+    assert ((out >= low) & (out <= high)).all(), (np.mean((out < low) | (out > high)), np.abs((out - ref) / size).max())
+
+
+def nearest_bf16(x):
+    """float64 to the nearest bfloat16 in one rounding, ties to even."""
+    _, e = np.frexp(x)
+    step = np.ldexp(1.0, e - 8)
+    return np.rint(x / step) * step
