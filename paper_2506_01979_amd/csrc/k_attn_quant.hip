@@ -282,6 +282,7 @@ struct Tiles {
 #pragma unroll
       for (int dt = 0; dt < NF; ++dt) o[rt][dt] *= f;
   }
+  // The largest finite one: an infinity in the tail's V stays in its own sums.
   __device__ __forceinline__ float largest_out() const {
     float top = 0.0f;
 #pragma unroll
@@ -289,7 +290,10 @@ struct Tiles {
 #pragma unroll
       for (int dt = 0; dt < NF; ++dt)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) top = fmaxf(top, fabsf(o[rt][dt][e]));
+        for (int e = 0; e < 4; ++e) {
+          const float x = fabsf(o[rt][dt][e]);
+          top = fmaxf(top, x < INFINITY ? x : 0.0f);
+        }
     for (int i = 32; i > 0; i >>= 1) top = fmaxf(top, __shfl_xor(top, i, 64));
     return top;
   }

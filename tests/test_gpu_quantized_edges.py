@@ -1,5 +1,5 @@
-"""GPU tests of the 8-bit cache where it can go wrong: the largest finite values
-and the bits of the softmax weights."""
+"""GPU tests of the 8-bit cache where it can go wrong: the largest finite values,
+the bits of the softmax weights and values that are not finite."""
 import numpy as np
 import pytest
 import torch
@@ -125,3 +125,27 @@ def nearest_bf16(x):
     _, e = np.frexp(x)
     step = np.ldexp(1.0, e - 8)
     return np.rint(x / step) * step
+
+
+@pytest.mark.parametrize("form", FORMATS)
+@pytest.mark.parametrize("nh,nkv,d,nb,tail,n,bad", [(4, 2, 64, 6, 9, 5, 3), (4, 2, 128, 12, 40, 33, 39), (128, 64, 64, 130, 9, 5, 3),
+                                                    (64, 64, 128, 130, 70, 20, 0)])
+@pytest.mark.parametrize("value", [np.inf, -np.inf, np.nan])
+def test_attend_value_not_finite_in_the_tail(api, form, nh, nkv, d, nb, tail, n, bad, value):
+    """One value of a committed tail slot that is not finite: every row attends to
+    it and shows it in that dimension, the others are what they are without it (with
+    many heads a wave goes on from the tail to blocks)."""
+    g = np.random.default_rng(nb + n)
+    parents = random_tree(g, n)
+    cfg, c, k, v, q = exact_cache(api, g, form, nh, nkv, d, nb, tail, parents)
+    say("attend, not finite in the tail", form, nh, nkv, d, nb, tail, n, bad, value)
+    without = attend(api, cfg, c, nb, tail, q, parents)
+    c.tail_v[0, 1, 17, bad] = value
+    out = attend(api, cfg, c, nb, tail, q, parents)
+    hit = slice(nh // nkv, 2 * (nh // nkv))
+    shown = torch.zeros(out.shape, dtype=torch.bool, device="cuda")
+    shown[:, hit, 17] = True
+    assert not torch.isfinite(out[shown]).any()
+    # the sums of a wave may be kept in another unit: float32 roundings, then one bfloat16 step
+    a, b = host(out[~shown]), host(without[~shown])
+    assert np.isfinite(a).all() and (np.abs(a - b) <= 2.0 ** -7 * np.abs(b) + 1e-5).all()
