@@ -47,6 +47,7 @@ namespace {
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kNW = 4;  // waves of a workgroup
 constexpr int kT = 64 * kNW;
@@ -83,6 +84,27 @@ __device__ __forceinline__ void split_f16(const float (&x)[8], f16x8 &hi, f16x8 
     lo[e] = (_Float16)fmaf((float)h[0], minus, x[e]);
     lo[e + 1] = (_Float16)fmaf((float)h[1], minus, x[e + 1]);
   }
+}
+
+// All ones in the halves of w that are not finite as bfloat16.
+__device__ __forceinline__ uint32_t not_finite(int w) {
+  return ((w & 0x7f80) == 0x7f80 ? 0xffffu : 0u) | ((w & 0x7f800000) == 0x7f800000 ? 0xffff0000u : 0u);
+}
+// Whether any value of a wave's fragments is; they are then zeros.
+template <int N>
+__device__ __forceinline__ bool take_not_finite(i32x4 (&f)[N]) {
+  u16x2 top = {0, 0};
+#pragma unroll
+  for (int i = 0; i < N; ++i)
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2, f[i][e] & 0x7fff7fff));
+  if (!__ballot(top[0] >= 0x7f80 || top[1] >= 0x7f80)) return false;
+#pragma unroll
+  for (int i = 0; i < N; ++i)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) f[i][e] &= (int)~not_finite(f[i][e]);
+  return true;
 }
 
 // Four codes to binary16, exactly.
@@ -384,6 +406,27 @@ struct Tiles {
       }
     }
   }
+  // NaN into the sums of dimension tile dt of every row that sees (vis(rt)) a key
+  // whose value in V's fragment is not finite.
+  template <class V>
+  __device__ __forceinline__ void show_not_finite(int dt, i32x4 v, const V &vis) {
+    i32x4 bad;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) bad[e] = (int)(not_finite(v[e]) & 0x3f803f80u);  // ones
+    if (!__ballot((bad[0] | bad[1] | bad[2] | bad[3]) != 0)) return;
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+      const uint32_t see = vis(rt);
+      i32x4 one;
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        one[e] = (int)(((see >> (2 * e)) & 1u ? 0x3f80u : 0u) | ((see >> (2 * e + 1)) & 1u ? 0x3f800000u : 0u));
+      const f32x4 n = mfma16(__builtin_bit_cast(bf16x8, bad), __builtin_bit_cast(bf16x8, one),
+                             f32x4{0.f, 0.f, 0.f, 0.f});
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[rt][dt][e] = n[e] > 0.0f ? NAN : o[rt][dt][e];
+    }
+  }
   // One step of 32 tail keys.  q(rt, j): bfloat16 query fragment; kfrag(i, j):
   // key tile i, k-step j; vfrag(dt); vis(rt): bit e of it, key 8 lg + e of the
   // step is visible to the lane's row.
@@ -539,16 +582,18 @@ __global__ __launch_bounds__(kT, 2) void k_attn_quant(QuantAttnArgs a, TreeMasks
         kf[i * KSD + j] = __builtin_amdgcn_raw_buffer_load_b128(tks, vo, j * 64, 0);
     }
   };
+  auto load_tail_v = [&](int u, int dt) {
+    const int key = (rg.t0 + u) * 32 + 8 * lg;
+    return __builtin_amdgcn_raw_buffer_load_b128(
+        tvs, key < nkeys ? ((16 * dt + lr) * a.tail_cap + key) * 2 : tbytes, 0, 0);
+  };
   auto load_v = [&](int u) {
     if (u >= nt) {
       if (u < nu) load_block(vf, vrs, u);
       return;
     }
-    const int key = (rg.t0 + u) * 32 + 8 * lg;
 #pragma unroll
-    for (int i = 0; i < NF; ++i)
-      vf[i] = __builtin_amdgcn_raw_buffer_load_b128(
-          tvs, key < nkeys ? ((16 * i + lr) * a.tail_cap + key) * 2 : tbytes, 0, 0);
+    for (int i = 0; i < NF; ++i) vf[i] = load_tail_v(u, i);
   };
   // the wave's first block, and the blocks' scales
   const int first = rg.b0 + (w < nt ? (w - nt) & (kNW - 1) : w - nt);
@@ -578,6 +623,13 @@ __global__ __launch_bounds__(kT, 2) void k_attn_quant(QuantAttnArgs a, TreeMasks
   tl.init();
   int u = w;
   float unscale = 1.0f;  // of the output sums
+  auto seen = [&](int rt, int k0) {
+    const int r = rg.rb * RB + rt * 16 + lr;
+    return tail_visible(sanc[r < R ? (int)(((float)r + 0.5f) * inv_g) : 0], k0, a.tail_len, nkeys);
+  };
+  // A tree row's V that is not finite must not reach the rows that do not see it, as 0
+  // times it is NaN: it is taken out of the products and shown afterwards.
+  bool bad = false;
   for (; u < nt; u += kNW) {
     const int k0 = (rg.t0 + u) * 32 + 8 * lg;  // this lane's 8 keys
     const bool all = (rg.t0 + u + 1) * 32 <= a.tail_len;
@@ -590,17 +642,20 @@ __global__ __launch_bounds__(kT, 2) void k_attn_quant(QuantAttnArgs a, TreeMasks
         for (int dt = 0; dt < NF; ++dt) vf[dt][e] &= keep;
       }
     }
+    if (!all) bad |= take_not_finite(vf);
     tl.tail([&](int rt, int j) { return as_bf16x8(*(const uint4 *)&sb[rt * 16 + lr][32 * j + 8 * lg]); },
             [&](int i, int j) { return __builtin_bit_cast(bf16x8, kf[i * KSD + j]); },
             [&](int dt) { return __builtin_bit_cast(bf16x8, vf[dt]); },
-            [&](int rt) {
-              if (all) return 0xffu;
-              const int r = rg.rb * RB + rt * 16 + lr;
-              return tail_visible(sanc[r < R ? (int)(((float)r + 0.5f) * inv_g) : 0], k0, a.tail_len, nkeys);
-            },
-            c, [&]() { load_k(u + kNW); });
+            [&](int rt) { return all ? 0xffu : seen(rt, k0); }, c, [&]() { load_k(u + kNW); });
     load_v(u + kNW);
   }
+  if (bad)
+    for (int s = w; s < nt; s += kNW) {
+      const int key = (rg.t0 + s) * 32 + 8 * lg;
+#pragma unroll
+      for (int dt = 0; dt < NF; ++dt)
+        tl.show_not_finite(dt, load_tail_v(s, dt), [&](int rt) { return seen(rt, key); });
+    }
   if (u < nu) {
     float vtop = sc.largest_v(a, rg.g, first, kNW, rg.b1);
     if (nt) {

@@ -6,6 +6,7 @@ import torch
 
 from gpu_util import say
 from oracle import quantized
+from paper_2506_01979_amd import synth
 from test_gpu_quantized import bf16, dev, host, random_tree
 
 pytestmark = pytest.mark.gpu
@@ -149,3 +150,61 @@ def test_attend_value_not_finite_in_the_tail(api, form, nh, nkv, d, nb, tail, n,
     # the sums of a wave may be kept in another unit: float32 roundings, then one bfloat16 step
     a, b = host(out[~shown]), host(without[~shown])
     assert np.isfinite(a).all() and (np.abs(a - b) <= 2.0 ** -7 * np.abs(b) + 1e-5).all()
+
+
+@pytest.mark.parametrize("form", FORMATS)
+@pytest.mark.parametrize("d,nb,tail,n", [(64, 6, 9, 20), (128, 12, 40, 33), (128, 130, 62, 129), (64, 0, 0, 12)])
+@pytest.mark.parametrize("value", [np.inf, np.nan])
+def test_attend_row_not_finite_off_the_path(api, form, d, nb, tail, n, value):
+    """A tree row whose K and V are not finite: the rows on whose path it stands show
+    it, the others are what they are without it."""
+    g = np.random.default_rng(nb + n)
+    parents = random_tree(g, n)
+    cfg, c, k, v, q = exact_cache(api, g, form, 4, 2, d, nb, tail, parents)
+    say("attend, not finite beside the path", form, d, nb, tail, n, value)
+    without = attend(api, cfg, c, nb, tail, q, parents)
+    bad = n // 2
+    c.tail_k[0, 0, tail + bad, 5] = value
+    c.tail_v[0, 0, 11, tail + bad] = value
+    c.tail_v[0, 1, :, tail + bad] = value
+    out = attend(api, cfg, c, nb, tail, q, parents)
+    sees = torch.from_numpy(on_path(parents)[:, bad].copy()).cuda()
+    assert 1 <= int(sees.sum()) < n
+    a, b = host(out[~sees]), host(without[~sees])
+    assert np.isfinite(a).all() and (np.abs(a - b) <= 2.0 ** -7 * np.abs(b) + 1e-5).all()
+    assert not torch.isfinite(out[sees][:, 2:]).any() and not torch.isfinite(out[sees][:, :2, 11]).any()
+
+
+@pytest.mark.parametrize("projections", [None, "int8"])
+def test_forward_with_a_row_not_finite(api, projections):
+    """A draft token whose embedding is not finite: its row and its descendants show it,
+    the others' logits, statistics and tail K/V are what they are without it."""
+    shape = synth.SHAPES["small_gqa_bf16"]
+    parents, nb, tail = synth.fork_parents(1, 3, 4), 2, 11
+    n, V = len(parents), shape.vocab
+    m = api.Model(shape, api.synth_tensors(shape), projections=projections)
+    g = torch.Generator(device="cuda").manual_seed(7)
+    c = api.QuantizedKV(m.cfg, 64 * nb, tail + n, "int8")
+    k, v = m.new_kv(64 * nb)
+    k.normal_(generator=g)
+    v.normal_(generator=g)
+    api.sb_kv_quantize(m.cfg, k, v, 0, c, 0, nb)
+    c.tail_k.normal_(generator=g)
+    c.tail_v.normal_(generator=g)
+    tokens = torch.arange(n, dtype=torch.int32, device="cuda")
+    ws = m.quantized_workspace(n, nb, tail)
+    bad, outs = 3, []
+    for value in (None, float("nan")):
+        if value is not None:
+            m.embed[bad, 5] = value
+        logits, stats = torch.empty((n, V), device="cuda"), api.new_stats(n)
+        say("forward, a row not finite", projections, value)
+        m.sb_verify_forward_quantized(c, nb, tail, tokens, parents, 1.0, logits, stats, ws)
+        torch.cuda.synchronize()
+        outs.append((logits, stats.clone(), c.tail_k[:, :, tail:tail + n].clone(), c.tail_v[..., tail:tail + n].clone()))
+    sees = torch.from_numpy(on_path(parents)[:, bad].copy()).cuda()
+    assert 2 <= int(sees.sum()) < n
+    (l0, s0, k0, v0), (l1, s1, k1, v1) = outs
+    assert torch.equal(l1[~sees], l0[~sees]) and torch.equal(s1[~sees], s0[~sees])
+    assert torch.equal(k1[:, :, ~sees], k0[:, :, ~sees]) and torch.equal(v1[..., ~sees], v0[..., ~sees])
+    assert torch.isfinite(l0).all() and not torch.isfinite(l1[sees]).any()
