@@ -496,7 +496,7 @@ struct Tiles {
 };
 
 // Which of the 8 tail keys from k0 (a multiple of 8) a row with ancestor mask
-// anc sees, as visible8 but without branches.
+// anc sees, as visible8 of k_attn.hip but without branches.
 __device__ __forceinline__ uint32_t tail_visible(const uint32_t *anc, int k0, int tail_len, int nkeys) {
   const int jt = k0 - tail_len, at = max(jt, 0), pre = min(max(-jt, 0), 8);
   const int wi = min(at >> 5, 7);
