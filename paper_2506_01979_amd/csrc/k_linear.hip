@@ -416,12 +416,7 @@ hipError_t launch_ring_tt(const LinearArgs &a, hipStream_t s) {
   return launch_ring<NT, 16>(a, s);
 }
 
-// Which of the two kernels, and with what: ring_tiles is 0 for k_linear with nt
-// weight tiles a workgroup and the token tiles in tblocks blocks, else the weight
-// tiles of a ring wave, over `splits` K ranges.
-struct LinearPlan {
-  int nt, tblocks, ring_tiles, splits;
-};
+}  // namespace
 
 // The kernel and its tiles by what a compute unit has to bring in, in KB (1 KB per
 // tile and k-step), as its fill rate bounds both kernels; a round of workgroups
@@ -476,8 +471,6 @@ LinearPlan linear_plan(int tiles, int ks, int n_tok) {
   }
   return p;
 }
-
-}  // namespace
 
 LinearGeom linear_geom(int m, int k) {
   LinearGeom g{};

@@ -343,6 +343,13 @@ struct LinearArgs {
   int32_t *part;  // linear_part_bytes of them: the sums of K ranges
   int vec, ttiles, tblocks, splits;  // filled in by the launch
 };
+// Which of the two kernels, and with what: ring_tiles is 0 for k_linear with nt
+// weight tiles a workgroup and the token tiles in tblocks blocks, else the weight
+// tiles of a ring wave, over `splits` K ranges.
+struct LinearPlan {
+  int nt, tblocks, ring_tiles, splits;
+};
+LinearPlan linear_plan(int tiles, int ks, int n_tok);
 // Bytes of the sums that a product of up to max_rows rows leaves for its join.
 size_t linear_part_bytes(int m, int k, int max_rows);
 hipError_t launch_linear(const LinearArgs &a, hipStream_t s);

@@ -1,11 +1,12 @@
 """GPU tests of the 8-bit projections where they can go wrong: the largest finite
-values."""
+values, and every form of their kernels that the rule takes at any size."""
 import numpy as np
 import pytest
 import torch
 
 from gpu_util import say
 from oracle import int8
+from linear_forms import CASES, form
 from test_gpu_int8 import bf16, product
 
 pytestmark = pytest.mark.gpu
@@ -49,3 +50,51 @@ def test_linear_largest_values(api, k, size):
         with np.errstate(over="ignore"):
             ref = int8.linear(x.float().numpy(), w.float().numpy(), dt)
         assert np.array_equal(got, ref) and (size == 1.0 or np.isfinite(ref).all())
+
+
+@pytest.mark.parametrize("m,k,ns", CASES)
+def test_linear_forms(api, m, k, ns):
+    """y bit for bit on 400 channels (all of fewer), the first and last among them, on a
+    workspace sized for the most rows and full of other bytes."""
+    g = torch.Generator(device="cuda").manual_seed(m + k)
+    w = torch.empty((m, k), dtype=torch.bfloat16, device="cuda").normal_(generator=g)
+    some = torch.arange(m) if m <= 400 else torch.cat([torch.arange(150), torch.randint(150, m - 150, (100,)),
+                                                       torch.arange(m - 150, m)])
+    packed = torch.full((api.sb_linear_packed_bytes(m, k),), 0x55, dtype=torch.uint8, device="cuda")
+    api.sb_linear_pack(w, packed)
+    wf = w[some.cuda()].float().cpu().numpy()
+    del w
+    ws = torch.full((api.sb_linear_workspace_bytes(m, k, 256),), 0xff, dtype=torch.uint8, device="cuda")
+    for n in ns:
+        say("linear", m, k, n, form(m, k, n))
+        x = torch.empty((n, k), dtype=torch.bfloat16, device="cuda").normal_(generator=g)
+        buf = torch.full((n * m + 64,), 7.0, device="cuda")
+        y = buf[:n * m].view(n, m)
+        api.sb_linear_quantized(packed, x, y, ws)
+        torch.cuda.synchronize()
+        assert (buf[n * m:] == 7.0).all()
+        assert np.array_equal(y[:, some.cuda()].cpu().numpy(), int8.linear(x.float().cpu().numpy(), wf))
+
+
+def test_linear_k_ranges_of_two_tiles_captured(api):
+    """K ranges of 256 channels' groups and their join, replayed beside eager calls on a
+    workspace of their own."""
+    m, k, n = 8192, 28672, 100
+    assert form(m, k, n) == ("ring", 2, 7, True)
+    g = torch.Generator(device="cuda").manual_seed(6)
+    packed = torch.empty(api.sb_linear_packed_bytes(m, k), dtype=torch.uint8, device="cuda")
+    api.sb_linear_pack(torch.empty((m, k), dtype=torch.bfloat16, device="cuda").normal_(generator=g), packed)
+    x0 = torch.empty((n, k), device="cuda").normal_(generator=g)
+    xd, y, y2 = x0.clone(), torch.zeros((n, m), device="cuda"), torch.zeros((n, m), device="cuda")
+    ws, ws2 = (torch.empty(api.sb_linear_workspace_bytes(m, k, n), dtype=torch.uint8, device="cuda") for _ in range(2))
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        api.sb_linear_quantized(packed, xd, y, ws)
+    for i in range(4):
+        xd.copy_(x0 * (3.0 if i % 2 else -1.0) + i)
+        y.zero_()
+        graph.replay()
+        api.sb_linear_quantized(packed, xd, y2, ws2)
+        torch.cuda.synchronize()
+        assert torch.equal(y, y2) and y.abs().max() > 0
