@@ -3,6 +3,7 @@ there for: the rules that choose them run on the host."""
 import math
 import random
 
+from attend_forms import MANY_BLOCKS, THREE_TILES, plan
 from linear_forms import CASES, form
 from paper_2506_01979_amd import synth
 
@@ -25,3 +26,12 @@ def test_linear_cases_take_every_form():
     tested = {form(m, k, n) for m, k, ns in CASES for n in ns}
     assert len(tested) > 80
     assert not set(taken) - tested, {f: taken[f] for f in set(taken) - tested}
+
+
+def test_attend_cases_take_their_forms():
+    assert all(plan(*c)[0] == 3 for c in THREE_TILES)
+    rows = [c[5] * (c[0] // c[1]) for c in THREE_TILES]
+    assert {-(-r // 16) % 3 for r in rows} == {0, 2}             # whole and ragged row blocks
+    assert {c[2] for c in THREE_TILES} == {64, 128}
+    assert {plan(*c)[0] for c in MANY_BLOCKS} == {1, 2, 3}
+    assert all(c[3] / (4 * plan(*c)[2]) > 64 for c in MANY_BLOCKS)

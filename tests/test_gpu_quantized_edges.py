@@ -1,13 +1,15 @@
 """GPU tests of the 8-bit cache where it can go wrong: the largest finite values,
-the bits of the softmax weights and values that are not finite."""
+the bits of the softmax weights, values that are not finite, and forms of the
+attention that only long prefixes take."""
 import numpy as np
 import pytest
 import torch
 
+from attend_forms import MANY_BLOCKS, THREE_TILES, plan
 from gpu_util import say
 from oracle import quantized
 from paper_2506_01979_amd import synth
-from test_gpu_quantized import bf16, dev, host, random_tree
+from test_gpu_quantized import bf16, check, dev, host, random_tree, reference
 
 pytestmark = pytest.mark.gpu
 
@@ -208,3 +210,31 @@ def test_forward_with_a_row_not_finite(api, projections):
     assert torch.equal(l1[~sees], l0[~sees]) and torch.equal(s1[~sees], s0[~sees])
     assert torch.equal(k1[:, :, ~sees], k0[:, :, ~sees]) and torch.equal(v1[..., ~sees], v0[..., ~sees])
     assert torch.isfinite(l0).all() and not torch.isfinite(l1[sees]).any()
+
+
+@pytest.mark.parametrize("form", FORMATS)
+@pytest.mark.parametrize("nh,nkv,d,nb,tail,n", THREE_TILES + MANY_BLOCKS)
+def test_attend_long(api, form, nh, nkv, d, nb, tail, n):
+    """Blocks of very different scales, a wave's largest V scale in its last ones: the
+    oracle's output on the first and the last KV head, to the bound of the other
+    attention tests."""
+    g = torch.Generator(device="cuda").manual_seed(nb + n)
+    parents = random_tree(np.random.default_rng(n), n)
+    say("attend, long", form, nh, nkv, d, nb, tail, n, plan(nh, nkv, d, nb, tail, n))
+    cfg, cut, keys = api.attention_config(1, nh, nkv, d), 64 * nb, 64 * nb + tail + n
+    size = torch.exp(torch.empty((2, 1, nkv, keys // 64 + 1, 1, 1), device="cuda").normal_(generator=g))
+    size[1, :, :, nb - 5:nb] *= 32.0
+    k, v = ((torch.empty((1, nkv, len(size[0, 0, 0]) * 64, d), device="cuda").normal_(generator=g).view(1, nkv, -1, 64, d)
+             * s).view(1, nkv, -1, d)[:, :, :keys].bfloat16() for s in size)
+    q = torch.empty((n, nh, d), device="cuda").normal_(generator=g).bfloat16()
+    c = api.QuantizedKV(cfg, cut, tail + n, form)
+    api.sb_kv_quantize(cfg, k[:, :, :cut].contiguous(), v[:, :, :cut].transpose(2, 3).contiguous(), 0, c, 0, nb)
+    c.tail_k[:, :, :tail + n] = k[:, :, cut:]
+    c.tail_v[:, :, :, :tail + n] = v[:, :, cut:].transpose(2, 3)
+    out = attend(api, cfg, c, nb, tail, q, parents)
+    G = nh // nkv
+    for h in (0, nkv - 1):
+        kk, vv = (np.concatenate([quantized.values(*quantized.quantize(host(x[0, h, :cut]), form)), host(x[0, h, cut:])])
+                  for x in (k, v))
+        heads = slice(h * G, (h + 1) * G)
+        check(out[:, heads], *reference(q[:, heads].cpu(), kk[None], vv[None], parents))
