@@ -256,6 +256,13 @@ def _ptr(t) -> int | None:
     return None if t is None else t.data_ptr()
 
 
+def _int32(n: int, what: str) -> int:
+    """A size for an int32 argument, which ctypes would cut to 32 bits."""
+    if not -2 ** 31 <= n < 2 ** 31:
+        raise ValueError(f"{what}: {n} does not fit an int32")
+    return n
+
+
 def _host_i32(a) -> tuple:
     arr = np.ascontiguousarray(np.asarray(a, dtype=np.int32))
     # byref of the first element: 0.6 us, arr.ctypes.data_as() 1.1; arr keeps
@@ -588,7 +595,7 @@ def sb_attend_quantized(cfg: ModelConfig, cache: QuantizedKV, layer: int, n_bloc
 
 
 def sb_linear_packed_bytes(m: int, k: int) -> int:
-    return int(lib.sb_linear_packed_bytes(m, k))
+    return int(lib.sb_linear_packed_bytes(_int32(m, "m"), _int32(k, "k")))
 
 
 def sb_linear_pack(w: torch.Tensor, packed: torch.Tensor, stream=None) -> None:
@@ -602,7 +609,7 @@ def sb_linear_pack(w: torch.Tensor, packed: torch.Tensor, stream=None) -> None:
 
 
 def sb_linear_workspace_bytes(m: int, k: int, max_rows: int) -> int:
-    return int(lib.sb_linear_workspace_bytes(m, k, max_rows))
+    return int(lib.sb_linear_workspace_bytes(_int32(m, "m"), _int32(k, "k"), _int32(max_rows, "max_rows")))
 
 
 def sb_linear_quantized(packed: torch.Tensor, x: torch.Tensor, y: torch.Tensor, ws: torch.Tensor,
@@ -623,7 +630,7 @@ def sb_linear_quantized(packed: torch.Tensor, x: torch.Tensor, y: torch.Tensor, 
     _need(packed, need, "packed")
     _need(ws, 0, "ws")
     handle = _stream_on(stream, packed, x, y, ws)
-    _check(lib.sb_linear_quantized(m, k, packed.data_ptr(), n, x.data_ptr(),
+    _check(lib.sb_linear_quantized(m, k, packed.data_ptr(), _int32(n, "x"), x.data_ptr(),
                                    SB_BF16 if x.dtype is torch.bfloat16 else SB_F32, y.data_ptr(),
                                    ws.data_ptr(), ws.nbytes, handle),
            "sb_linear_quantized")
@@ -634,9 +641,10 @@ def sb_count_tokens(tokens: torch.Tensor, counts: torch.Tensor, accumulate: bool
     """tokens int32 [n]; counts int32 [vocab]."""
     _need(tokens, 0, "tokens", torch.int32)
     _need(counts, 0, "counts", torch.int32)
+    vocab, n = _int32(counts.numel(), "counts"), _int32(tokens.numel(), "tokens")
     handle = _stream_on(stream, tokens, counts)
-    _check(lib.sb_count_tokens(counts.numel(), tokens.numel(), tokens.data_ptr(), int(accumulate),
-                               counts.data_ptr(), handle), "sb_count_tokens")
+    _check(lib.sb_count_tokens(vocab, n, tokens.data_ptr(), int(accumulate), counts.data_ptr(), handle),
+           "sb_count_tokens")
 
 
 def sb_count_step(tokens: torch.Tensor, result: torch.Tensor, counts: torch.Tensor,
@@ -645,9 +653,10 @@ def sb_count_step(tokens: torch.Tensor, result: torch.Tensor, counts: torch.Tens
     _need(tokens, 4, "tokens", torch.int32)
     _need(result, STEP_RESULT_INTS * 4, "result", torch.int32)
     _need(counts, 4, "counts", torch.int32)
+    vocab, n = _int32(counts.numel(), "counts"), _int32(tokens.numel(), "tokens")
     handle = _stream_on(stream, tokens, result, counts)
-    _check(lib.sb_count_step(counts.numel(), tokens.numel(), tokens.data_ptr(), result.data_ptr(),
-                             counts.data_ptr(), handle), "sb_count_step")
+    _check(lib.sb_count_step(vocab, n, tokens.data_ptr(), result.data_ptr(), counts.data_ptr(), handle),
+           "sb_count_step")
 
 
 class LogitRules:
@@ -669,7 +678,8 @@ class LogitRules:
             _need(mask, 0, "mask")
         rows = 1 if mask is None or mask.dim() == 1 else mask.shape[0]
         self.struct = LogitRulesStruct(_ptr(prompt), _ptr(output), repetition, presence, frequency,
-                                       _ptr(bias), _ptr(mask), 0 if rows == 1 else mask.shape[1])
+                                       _ptr(bias), _ptr(mask),
+                                       0 if rows == 1 else _int32(mask.shape[1], "mask"))
 
     def _check(self, vocab: int, n_rows: int) -> None:
         for t, name in zip(self.tensors[:3], ("prompt", "output", "bias")):
@@ -685,7 +695,7 @@ class LogitRules:
 
 
 def sb_shape_workspace_bytes(vocab: int, n_rows: int) -> int:
-    return int(lib.sb_shape_workspace_bytes(vocab, n_rows))
+    return int(lib.sb_shape_workspace_bytes(_int32(vocab, "vocab"), _int32(n_rows, "n_rows")))
 
 
 def sb_shape_logits(rules: LogitRules, tokens: torch.Tensor, parents, logits: torch.Tensor,
@@ -693,7 +703,7 @@ def sb_shape_logits(rules: LogitRules, tokens: torch.Tensor, parents, logits: to
                     stream=None) -> None:
     """logits and out float32 [n_rows][vocab] (may be one tensor); tokens int32 [n_rows]."""
     par, pp = _host_i32(parents)
-    n, v = len(par), logits.shape[-1]
+    n, v = len(par), _int32(logits.shape[-1], "logits")
     _need(tokens, n * 4, "tokens", torch.int32)
     _need(logits, n * v * 4, "logits", torch.float32)
     if out.shape[-1] != v:
