@@ -10,13 +10,15 @@
 // in the loop, every code is converted once per row block, and the waves' sums
 // meet in LDS after the last step.  (Waves that share the rows instead, with the
 // steps in a ring of LDS buffers, met at a barrier a step and read every fragment
-// once per wave: 81 us where this form takes 49, 13B, 129 rows, prefix 8192.)
+// once per wave: 81 us where this form took 49, 13B, 129 rows, prefix 8192, both with
+// weights of one part.)
 //
 // What bounds it.  Few rows: the launch, the first loads' latency and the merge
-// (68M, 1 row, 300 keys: 5.5 + 2.5 us for 1 MB; 70B, 1 row, 32773 keys: 15.5 + 4 us
-// where the 67 MB alone take 14).  Many rows: the vector unit -- 590 instructions
-// a block with three row tiles, 3.6 kcycles of a wave with another on the same
-// SIMD, against 1.5 in the matrix unit (13B, 129 rows, prefix 8192: 42 us + 5).
+// (68M, 1 row, 300 keys: 5.7 + 2.5 us for 1 MB; 70B, 1 row, 32773 keys: 15.5 + 4 us
+// where the 67 MB alone take 14).  Many rows: the vector and the matrix unit, which
+// two waves a SIMD hardly overlap -- 510 (int8 638) and 144 instructions a block with
+// three row tiles; 13B, 129 rows, prefix 8192: busy for 59 and 35 of the 98 kcycles
+// that a wave lives, 57 us with the merge.
 //
 // An 8-bit block (64 keys): its codes come in operand order, 16 bytes per lane
 // and fragment, straight into registers, and are widened to binary16 there,
@@ -752,17 +754,19 @@ hipError_t launch_df(const QuantAttnArgs &a, const TreeMasks &tree, int rt, hipS
 
 }  // namespace
 
-// Row tiles of a wave and key ranges (attention and merge, by the row tiles of a
+// Row tiles of a wave and key ranges (attention and merge, us, by the row tiles of a
 // KV head):
 //  - up to three tiles (six at head_dim 64) one each, so that the waves start and
-//    end sooner: 13B, 33 rows, prefix 4096 19.2 us against 20.4 with two a wave
-//    and 22.4 with three; 68M, 65 rows 12.3 against 13.9;
-//  - more, two, which halves the codes' conversions: 13B, 65 rows 25.1 against
-//    26.7; 70B, 33 rows 20.9 against 21.8;
-//  - three where the range is long and they waste no more of a row block: 13B,
-//    129 rows, prefix 8192 48.0 (int8 51.8) against 51.4 (55.9) with two;
+//    end sooner: 13B, 33 rows, prefix 4096 20.7 against 21.6 with two a wave and
+//    29.4 with three; 68M, 65 rows 9.2 against 10.4 and 12.5;
+//  - more, two, which halves the codes' conversions: 13B, 65 rows 26.9 against 27.8
+//    with one; 13B, 129 rows 37.1 against 43.9 (70B, 33 rows 23.7 against 22.5);
+//  - three where the prefix is long and they waste no more of a row block: prefix
+//    8192, 13B, 129 rows 57.7 (int8 61.0) against 61.9 (67.6) with two; 70B, 129
+//    rows 85.5 against 105.5 (70B, 33 rows, where they leave a quarter of the compute
+//    units' places empty, 35.4 against 28.0; 7B, 129 rows 51.0 against 47.9);
 //  - two workgroups per compute unit, one where that takes more than eight ranges
-//    of a KV head (70B, 5 rows: 10 ranges 11.1 us, 16 11.8): what a range writes
+//    of a KV head (70B, 5 rows: 10 ranges 13.3, 16 14.2): what a range writes
 //    for the merge grows with them.
 QuantAttnPlan quant_attn_plan(int n_kv, int head_dim, int n_blocks, int tail_keys, int rows) {
   QuantAttnPlan p{};

@@ -15,7 +15,7 @@
 // - k_linear_ring, many rows: 128 or 256 channels and all rows per workgroup, so
 //   that activations are read once per that many channels, through a ring of LDS
 //   stages that its waves share; the weights, each wave's own, straight to
-//   registers.  57344 x 8192, 129 rows: 96 us, 5.2 TB/s (k_linear: 172).
+//   registers.  57344 x 8192, 129 rows: 91 us, 5.2 TB/s (k_linear: 171).
 #include <math.h>
 
 #include "sb_internal_fwd.h"
@@ -428,14 +428,15 @@ hipError_t launch_ring_tt(const LinearArgs &a, hipStream_t s) {
 // The ring's bytes count 1.3 times (1.25 with two tiles a wave: stages and
 // barriers), K ranges 300 KB (the join's launch) and twice their sums.  (45000 x
 // 5120 with one tile a wave, or k_linear, against two: 49 rows 58.7 / 48.2, 65 rows
-// 63.2 / 50.2.)  Measured, k_linear / ring, us:
-//   rows                   17           33            65            129
-//   4096 x 4096         9.3 / 14.0  10.4 / 16.0   12.2 / 18.1   14.0 / 22.7
-//   12288 x 4096       13.6 / 17.1  15.1 / 18.6   18.0 / 20.3   26.1 / 26.1
-//   22016 x 4096       20.3 / 24.6  22.6 / 26.2   28.1 / 28.3   44.1 / 33.9
-//   5120 x 13824       26.4 / 22.9  29.9 / 24.5   36.6 / 28.3   43.6 / 34.7
-//   8192 x 28672       51.3 / 53.6  61.1 / 52.4   76.3 / 61.0  100   / 76.8
-//   57344 x 8192       82.2 / 95.2  90.4 / 86.7  115   / 85.0  178   / 98
+// 63.2 / 50.2.)  Measured, k_linear / the ring with one / with two tiles a wave, with the
+// rows' quantisation, us:
+//   rows                    17                  33                  65                  129
+//   4096 x 4096      9.3 / 13.7 / 15.5  10.4 / 15.7 / 17.4  12.3 / 18.3 / 20.2  14.0 / 23.4 / 26.8
+//   12288 x 4096    14.5 / 18.0 / 21.7  15.4 / 19.5 / 24.0  18.0 / 22.7 / 25.5  26.5 / 28.7 / 31.3
+//   22016 x 4096    21.2 / 25.1 / 31.4  22.5 / 26.2 / 33.0  28.0 / 28.3 / 34.2  43.7 / 33.6 / 41.5
+//   5120 x 13824    26.6 / 22.7 / 26.8  30.1 / 24.6 / 29.3  36.5 / 28.3 / 34.0  43.3 / 34.8 / 39.2
+//   8192 x 28672    53.7 / 50.8 / 53.0  59.2 / 52.8 / 54.5  74.8 / 60.6 / 60.4   101 / 74.2 / 75.1
+//   57344 x 8192    85.4 / 86.4 / 86.2  89.5 / 88.1 / 87.9   114 / 94.9 / 85.4   177 / 116  / 95.6
 // One token tile is always k_linear's.
 LinearPlan linear_plan(int tiles, int ks, int n_tok) {
   LinearPlan p{};

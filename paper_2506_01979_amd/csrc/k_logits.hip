@@ -7,8 +7,9 @@
 //   l -= freq * c;  c > 0: l -= pres;  l += bias[v];  not allowed: -inf.
 // Counts are whole numbers below 2^24, exact in float32.
 //
-// The counts are bound by their launch: 33 tokens of 32000 2.6 us, 32768 of 128256
-// 4.8 us.  The rules: at k_shape_logits.
+// The counts of some 30000 tokens and fewer are bound by their launch: 33 tokens of
+// 32000 2.6 us, 32768 of 128256 4.6 us; longer lists by the slices that each read all
+// of them, 2^20 tokens of 128256 86 us.  The rules: at k_shape_logits.
 #pragma clang fp contract(off)
 
 #include <limits.h>
@@ -122,8 +123,9 @@ __device__ __forceinline__ bool plain(float y, float r) {
   return __float_as_uint(y * r) - 0x21800000u < 0x71800000u - 0x21800000u;
 }
 
-// e^t for t <= 0 (any t below -200 or NaN: about e^-200): 2^p by the hardware, 1
-// ulp, with p = t log2(e) rounded and what it leaves put back.
+// e^t for t <= 0: 2^p by the hardware, 1 ulp, with p = t log2(e) rounded and what it
+// leaves put back.  0 for t below -200 and NaN, which -200 stands for: e^-200 is below
+// float32, and no infinity or NaN reaches what is put back.
 __device__ __forceinline__ float exp_below(float t) {
   t = fmaxf(t, -200.0f);
   const float p = t * 0x1.715476p+0f;
@@ -176,8 +178,8 @@ __global__ __launch_bounds__(SB_MAX_ROWS) void k_tree_paths(TreeArg tree, uint64
 //
 // Bound by the logits' way in and out and by the vector unit: 37 rows of 128256
 // under every rule are 38 MB of them, 8 us at a copy's rate, and some 45 instructions
-// per token; 11 us and the finishing pass's 4.  Tried and not kept: slices of a
-// workgroup with barriers between its waves (14.5), 16 tokens a lane (more registers,
+// per token; 14.4 us and the finishing pass's 3.9.  Tried and not kept: slices of a
+// workgroup with barriers between its waves (18.5), 16 tokens a lane (more registers,
 // 0.3 to 1.5 us slower), several rows per wave with the counts read once (the same or
 // slower), the penalties on a compacted list of seen tokens (the same at 37 rows,
 // slower above).
