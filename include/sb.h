@@ -711,8 +711,9 @@ size_t sb_attend_workspace_bytes(const sb_model_config *cfg, int32_t max_rows, i
  *   layer: which layer of the caches.
  * softmax(q k / sqrt(head_dim)) v with float32 sums and statistics; over the
  * 8-bit blocks q enters the products as binary16 scaled per row (exact down to
- * 2^-28 of its largest magnitude) and the softmax weights to 22 bits, over the
- * tail the weights to 16.  A tree row whose K or V is not finite shows in the
+ * 2^-28 of its largest magnitude) and the softmax weights to 22 bits, in steps no
+ * finer than 2^-40 of what the KV head's largest V scale would give a weight of 1;
+ * over the tail the weights to 16.  A tree row whose K or V is not finite shows in the
  * rows on whose path it stands, and in no other.
  * n_blocks and tail_len may be 0.  64 n_blocks <= kv->capacity, tail_len +
  * n_rows <= kv->tail.capacity (SB_ERR_CAPACITY), tail_len + n_rows <= 65536
