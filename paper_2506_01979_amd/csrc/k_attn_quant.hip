@@ -31,8 +31,9 @@
 // so that w <= 2^15 in two binary16 parts, a product each, keeps 22 bits, down to steps
 // of 2^-40 of the largest weight: no less than the two bfloat16 parts of k_attn.hip.
 // (One part, 11 bits, moves 9 % of the bfloat16 outputs by a step; 13B, 129 rows,
-// prefix 8192 49.6 us with it, 57.0 with two; 7B, 33 rows 14.2 and 14.4.)  Q enters as binary16 scaled by a power of two per
-// row (largest magnitude in [2^14, 2^15)): exact for elements down to 2^-28 of it.
+// prefix 8192 49.6 us with it, 57.0 with two; 7B, 33 rows 14.2 and 14.4.)  Q enters as
+// binary16 scaled by a power of two per row (largest magnitude in [2^14, 2^15)): exact
+// for elements down to 2^-28 of it.
 // l sums the unrounded float32 w.
 //
 // A tail step (32 keys) is computed as in k_attn.hip: bfloat16 Q, K and V, the
